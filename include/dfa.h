@@ -201,6 +201,110 @@ dfa_status dfa_module_step(int code, const void* X, const void* Wqkv, const void
                            const void* bo, void* Q, void* K, void* V, void* O, void* R, void* Y, void* Ycache,
                            int B, int H, int L, int d, int w, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * The block around the attention module: layer norm in front of the
+ * projections, the linear layers behind and beside them, and the rotary
+ * positions between the QKV projection and attention.
+ *
+ * The conventions above hold (streams, memory, errors, capture, 16-byte
+ * alignment of every tensor), and in addition:
+ *   Stream types  the residual stream, which X of a layer norm and Y and the
+ *                 residual of a linear layer belong to, is bf16 or fp32.
+ *   Vectors       weight, bias, gate, mean, rstd, their gradients and pos are
+ *                 fp32 and need 4-byte alignment only.  weight, bias and gate of
+ *                 a layer norm or linear layer may differ per batch entry: row b
+ *                 begins `stride` elements behind row b - 1, so that slices of
+ *                 a [B][6C] modulation are taken as they are; stride 0 is one
+ *                 row for all.
+ *   Sizes         B * L <= 2^30 tokens and 2^40 elements per tensor; others
+ *                 below.  Sizes need no divisor: rows that 16 bytes do not
+ *                 divide are read at their own alignment.
+ *   Bits          Equal calls give equal bits; no sum uses atomics. */
+
+/* Element types of the residual stream. */
+enum { DFA_BF16 = 0, DFA_F32 = 1 };
+
+/* Layer norm of every token over its C features, with the affine weights of a
+ * plain norm or the modulation of a diffusion transformer:
+ *   Y = (X - mean) * rstd * (weight + weight_offset) + bias
+ * with mean and variance (divisor C) over the token's features in fp32, the
+ * variance summed over (X - mean)^2, and rstd = 1 / sqrt(variance + eps).
+ *   X [B][L][C] of x_type, Y [B][L][C] bf16
+ *   weight, bias   NULL (factor 1, whatever weight_offset; no bias), or rows of C
+ *   weight_offset  0 for plain weights, 1 for a modulation's 1 + scale
+ *   mean, rstd     fp32 [B][L], what the backward pass reads; each may be NULL
+ * C <= 16384 (else DFA_ERR_UNSUPPORTED); eps >= 0.  Y must not overlap X. */
+dfa_status dfa_layer_norm(const void* X, const void* weight, const void* bias, void* Y, void* mean, void* rstd,
+                          int x_type, int B, int L, int C, int64_t weight_stride, int64_t bias_stride,
+                          float weight_offset, float eps, hipStream_t stream);
+
+/* Its gradients.  With xh = (X - mean) * rstd and g = dY * (weight + weight_offset):
+ *   dX      = rstd * (g - mean_C(g) - xh * mean_C(g * xh))
+ *   dweight = sum over tokens of dY * xh,   dbias = sum over tokens of dY
+ *   dY [B][L][C] bf16; X and dX [B][L][C] of x_type; mean, rstd as the forward
+ *   pass wrote them; weight as there
+ *   dweight, dbias  fp32 [groups][C], each may be NULL.  groups = 1 sums over
+ *                   the whole batch (the gradient of a row that it shares),
+ *                   groups = B (at most 2^22) over each entry's tokens.
+ *   workspace       DEVICE buffer, 16-byte aligned, of at least
+ *                   dfa_layer_norm_backward_workspace_bytes() bytes (NULL is
+ *                   fine where that is 0 or both gradients are NULL); calls
+ *                   that share it must not overlap in time
+ * The sums run in fp32 over a fixed split of the tokens, which are then added
+ * in a fixed order in fp32. */
+dfa_status dfa_layer_norm_backward(const void* dY, const void* X, const void* weight, const void* mean,
+                                   const void* rstd, void* dX, void* dweight, void* dbias, void* workspace,
+                                   size_t workspace_bytes, int x_type, int B, int L, int C, int64_t weight_stride,
+                                   float weight_offset, int groups, hipStream_t stream);
+
+/* Bytes of DEVICE workspace dfa_layer_norm_backward needs (0 for bad sizes). */
+size_t dfa_layer_norm_backward_workspace_bytes(int B, int L, int C, int groups);
+
+/* Activations of a linear layer. */
+enum {
+    DFA_ACT_NONE = 0,
+    DFA_ACT_GELU = 1,        /* z * Phi(z), Phi the normal distribution function */
+    DFA_ACT_GELU_TANH = 2,   /* z / 2 * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) */
+    DFA_ACT_SILU = 3         /* z / (1 + exp(-z)) */
+};
+
+/* Linear layer with its whole epilogue in one pass:
+ *   Y = residual + gate * act(X W^T + bias)
+ * with fp32 accumulation and epilogue and one rounding, to y_type.
+ *   X         bf16 [B][H][L][K / H]: H = 1 is a token-major [B][L][K] tensor, H > 1
+ *             the output of the attention path, read as its merged heads
+ *             (K / H in {64, 72}, else DFA_ERR_UNSUPPORTED)
+ *   W         bf16 [N][K]; bias fp32 [N] or NULL
+ *   gate      rows of N, or NULL (factor 1)
+ *   residual  [B][L][N] of y_type, or NULL (0); it may be Y itself (the stream
+ *             updated in place) but must not overlap it otherwise
+ *   Y         [B][L][N] of y_type; must not overlap X, W, bias or gate
+ * K, N <= 2^20. */
+dfa_status dfa_linear(const void* X, const void* W, const void* bias, const void* gate, const void* residual, void* Y,
+                      int act, int y_type, int B, int L, int H, int K, int N, int64_t gate_stride,
+                      hipStream_t stream);
+
+/* Rotary positions over several axes (time, height, width).  The first
+ * sections[0] dims of a head rotate by the token's position along axis 0, the
+ * next sections[1] by axis 1, and so on; dims behind the last section stay as
+ * they are.  Pair i of a section of n dims turns by theta = pos * base^(-2i / n):
+ *   (x, y) -> (x cos theta - y sin theta, x sin theta + y cos theta)
+ *   Q, Qout      bf16 [B][Hq][L][d]; K, Kout bf16 [B][Hk][L][d] (both NULL, and
+ *                Hk = 0: Q alone).  An output may be its input (in place) but
+ *                must not overlap any other tensor of the call.
+ *   pos          fp32 [L][naxes], or one such table per batch entry,
+ *                pos_stride elements apart (0: one for all).  A position may be
+ *                fractional; its angle is reduced in fp64.
+ *   sections     HOST array of naxes even numbers >= 2, of sum <= d
+ *   interleaved  nonzero: the pairs of a section are dims (2i, 2i + 1), else
+ *                (i, i + n / 2)
+ *   inverse      nonzero: turn by -theta, which undoes the rotation and takes
+ *                the gradients of Qout and Kout to those of Q and K
+ * d even, 2 <= d <= 256 (else DFA_ERR_UNSUPPORTED); 1 <= naxes <= 4; base > 0. */
+dfa_status dfa_rope(const void* Q, const void* K, void* Qout, void* Kout, const void* pos, const int32_t* sections,
+                    int naxes, double base, int interleaved, int inverse, int B, int Hq, int Hk, int L, int d,
+                    int64_t pos_stride, hipStream_t stream);
+
 /* Mean relative absolute error of the plan search (Sec. 3.5):
  *   L(A, B) = mean_i clip(|A_i - B_i| / (max(|A_i|, |B_i|) + 1e-6), 0, 10)
  * over n bf16 elements (DEVICE pointers, 16-byte aligned).  The result is

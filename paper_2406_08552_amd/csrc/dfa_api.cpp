@@ -462,6 +462,252 @@ dfa_status dfa_module_step(int code, const void* X, const void* Wqkv, const void
 }
 
 // ---------------------------------------------------------------------------
+// The block around the attention module: layer norm, linear layer, rotary positions
+// ---------------------------------------------------------------------------
+namespace {
+
+dfa_status check_vector(const void* p, const char* name, bool required = false) {
+    if (!p) return required ? fail(DFA_ERR_INVALID_ARG, "%s is NULL", name) : DFA_OK;
+    if ((uintptr_t)p & 3u) return fail(DFA_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+    return DFA_OK;
+}
+
+dfa_status check_type(int type, const char* name) {
+    if (type != DFA_BF16 && type != DFA_F32) return fail(DFA_ERR_INVALID_ARG, "unknown %s %d", name, type);
+    return DFA_OK;
+}
+
+size_t type_bytes(int type) { return type == DFA_F32 ? 4 : 2; }
+
+// tokens x width elements of one tensor within the limits
+dfa_status check_tokens(int B, int L, int width, const char* name) {
+    if (B <= 0 || L <= 0 || width <= 0)
+        return fail(DFA_ERR_INVALID_ARG, "sizes must be positive (B=%d L=%d %s=%d)", B, L, name, width);
+    const long long tokens = (long long)B * L;
+    if (tokens > (1LL << 30)) return fail(DFA_ERR_INVALID_ARG, "B*L=%lld tokens is too large (at most 2^30)", tokens);
+    if ((unsigned long long)tokens * width > (1ULL << 40))
+        return fail(DFA_ERR_INVALID_ARG, "tensor of %llu elements is too large", (unsigned long long)tokens * width);
+    return DFA_OK;
+}
+
+// rows of `width` values, one per batch entry (stride) or one for all (0)
+dfa_status check_rows(const void* p, int64_t stride, int B, int width, const char* name, Region* r) {
+    *r = Region{nullptr, 0, name};
+    if (!p) return DFA_OK;
+    dfa_status st;
+    if ((st = check_vector(p, name)) != DFA_OK) return st;
+    if (stride < 0 || stride > (1LL << 40) / B)
+        return fail(DFA_ERR_INVALID_ARG, "%s stride %lld is out of range", name, (long long)stride);
+    *r = Region{p, ((size_t)(B - 1) * (size_t)stride + width) * 4, name};
+    return DFA_OK;
+}
+
+dfa::Rows rows_of(const void* p, int64_t stride) { return dfa::Rows{(const float*)p, p ? (long long)stride : 0}; }
+
+dfa_status check_norm(int x_type, int B, int L, int C) {
+    dfa_status st;
+    if ((st = check_type(x_type, "x_type")) != DFA_OK) return st;
+    if ((st = check_tokens(B, L, C, "C")) != DFA_OK) return st;
+    if (C > dfa::NORM_C_MAX)
+        return fail(DFA_ERR_UNSUPPORTED, "layer norm over C=%d features is not built (at most %d)", C, dfa::NORM_C_MAX);
+    return DFA_OK;
+}
+
+}  // namespace
+
+dfa_status dfa_layer_norm(const void* X, const void* weight, const void* bias, void* Y, void* mean, void* rstd,
+                          int x_type, int B, int L, int C, int64_t weight_stride, int64_t bias_stride,
+                          float weight_offset, float eps, hipStream_t stream) {
+    dfa_status st;
+    if ((st = check_norm(x_type, B, L, C)) != DFA_OK) return st;
+    if (!(eps >= 0.f)) return fail(DFA_ERR_INVALID_ARG, "eps=%g must be >= 0", (double)eps);
+    if ((st = check_ptr(X, "X")) != DFA_OK) return st;
+    if ((st = check_ptr(Y, "Y")) != DFA_OK) return st;
+    if ((st = check_vector(mean, "mean")) != DFA_OK) return st;
+    if ((st = check_vector(rstd, "rstd")) != DFA_OK) return st;
+    const size_t tokens = (size_t)B * L, elems = tokens * C;
+    Region ins[3] = {{X, elems * type_bytes(x_type), "X"}};
+    if ((st = check_rows(weight, weight_stride, B, C, "weight", &ins[1])) != DFA_OK) return st;
+    if ((st = check_rows(bias, bias_stride, B, C, "bias", &ins[2])) != DFA_OK) return st;
+    const Region outs[] = {{Y, elems * 2, "Y"}, {mean, tokens * 4, "mean"}, {rstd, tokens * 4, "rstd"}};
+    if ((st = check_regions(outs, 3, ins, 3)) != DFA_OK) return st;
+    dfa::NormLaunch a{};
+    a.X = X;
+    a.weight = rows_of(weight, weight_stride);
+    a.bias = rows_of(bias, bias_stride);
+    a.offset = weight_offset;
+    a.eps = eps;
+    a.Y = Y;
+    a.mean = (float*)mean;
+    a.rstd = (float*)rstd;
+    a.x_f32 = x_type == DFA_F32;
+    a.B = B;
+    a.L = L;
+    a.C = C;
+    return hip_status(dfa::launch_layer_norm(a, stream), "layer norm launch");
+}
+
+size_t dfa_layer_norm_backward_workspace_bytes(int B, int L, int C, int groups) {
+    if (check_norm(DFA_BF16, B, L, C) != DFA_OK || (groups != 1 && groups != B) || groups > dfa::NORM_GROUPS_MAX) return 0;
+    return dfa::norm_grad_partials(B, L, C, groups) * 4;
+}
+
+dfa_status dfa_layer_norm_backward(const void* dY, const void* X, const void* weight, const void* mean,
+                                   const void* rstd, void* dX, void* dweight, void* dbias, void* workspace,
+                                   size_t workspace_bytes, int x_type, int B, int L, int C, int64_t weight_stride,
+                                   float weight_offset, int groups, hipStream_t stream) {
+    dfa_status st;
+    if ((st = check_norm(x_type, B, L, C)) != DFA_OK) return st;
+    if (groups != 1 && groups != B)
+        return fail(DFA_ERR_INVALID_ARG, "groups=%d must be 1 or the batch (B=%d)", groups, B);
+    if (groups > dfa::NORM_GROUPS_MAX)
+        return fail(DFA_ERR_INVALID_ARG, "groups=%d is too large (at most 2^22)", groups);
+    if ((st = check_ptr(dY, "dY")) != DFA_OK) return st;
+    if ((st = check_ptr(X, "X")) != DFA_OK) return st;
+    if ((st = check_ptr(dX, "dX")) != DFA_OK) return st;
+    if ((st = check_vector(mean, "mean", true)) != DFA_OK) return st;
+    if ((st = check_vector(rstd, "rstd", true)) != DFA_OK) return st;
+    if ((st = check_vector(dweight, "dweight")) != DFA_OK) return st;
+    if ((st = check_vector(dbias, "dbias")) != DFA_OK) return st;
+    const bool sums = dweight || dbias;
+    const size_t need = sums ? dfa::norm_grad_partials(B, L, C, groups) * 4 : 0;
+    if (need) {
+        if ((st = check_ptr(workspace, "workspace")) != DFA_OK) return st;
+        if (workspace_bytes < need)
+            return fail(DFA_ERR_INVALID_ARG, "workspace of %zu bytes is too small (%zu needed)", workspace_bytes, need);
+    }
+    const size_t tokens = (size_t)B * L, elems = tokens * C, wide = elems * type_bytes(x_type);
+    Region ins[5] = {{dY, elems * 2, "dY"}, {X, wide, "X"}, {mean, tokens * 4, "mean"}, {rstd, tokens * 4, "rstd"}};
+    if ((st = check_rows(weight, weight_stride, B, C, "weight", &ins[4])) != DFA_OK) return st;
+    const Region outs[] = {{dX, wide, "dX"},
+                           {dweight, (size_t)groups * C * 4, "dweight"},
+                           {dbias, (size_t)groups * C * 4, "dbias"},
+                           {need ? workspace : nullptr, need, "workspace"}};
+    if ((st = check_regions(outs, 4, ins, 5)) != DFA_OK) return st;
+    dfa::NormGradLaunch a{};
+    a.dY = dY;
+    a.X = X;
+    a.weight = rows_of(weight, weight_stride);
+    a.offset = weight_offset;
+    a.mean = (const float*)mean;
+    a.rstd = (const float*)rstd;
+    a.dX = dX;
+    a.dweight = (float*)dweight;
+    a.dbias = (float*)dbias;
+    a.partial = (float*)workspace;
+    a.x_f32 = x_type == DFA_F32;
+    a.B = B;
+    a.L = L;
+    a.C = C;
+    a.groups = groups;
+    return hip_status(dfa::launch_layer_norm_backward(a, stream), "layer norm backward launch");
+}
+
+dfa_status dfa_linear(const void* X, const void* W, const void* bias, const void* gate, const void* residual, void* Y,
+                      int act, int y_type, int B, int L, int H, int K, int N, int64_t gate_stride,
+                      hipStream_t stream) {
+    dfa_status st;
+    if (act < DFA_ACT_NONE || act > DFA_ACT_SILU) return fail(DFA_ERR_INVALID_ARG, "unknown activation %d", act);
+    if ((st = check_type(y_type, "y_type")) != DFA_OK) return st;
+    if ((st = check_tokens(B, L, K, "K")) != DFA_OK) return st;
+    if ((st = check_tokens(B, L, N, "N")) != DFA_OK) return st;
+    if (K > (1 << 20) || N > (1 << 20))
+        return fail(DFA_ERR_INVALID_ARG, "K=%d or N=%d is too large (at most 2^20)", K, N);
+    if (H <= 0 || K % H) return fail(DFA_ERR_INVALID_ARG, "K=%d is not a multiple of H=%d heads", K, H);
+    if (H > 1 && !dfa::head_dim_supported(K / H))
+        return fail(DFA_ERR_UNSUPPORTED, "head dim K/H=%d is not built (supported: 64, 72)", K / H);
+    if ((st = check_ptr(X, "X")) != DFA_OK) return st;
+    if ((st = check_ptr(W, "W")) != DFA_OK) return st;
+    if ((st = check_vector(bias, "bias")) != DFA_OK) return st;
+    if (residual && (st = check_ptr(residual, "residual")) != DFA_OK) return st;
+    if ((st = check_ptr(Y, "Y")) != DFA_OK) return st;
+    const size_t tokens = (size_t)B * L, out = tokens * N * type_bytes(y_type);
+    Region ins[5] = {{X, tokens * K * 2, "X"},
+                     {W, (size_t)N * K * 2, "W"},
+                     {bias, (size_t)N * 4, "bias"},
+                     {residual == Y ? nullptr : residual, out, "residual"}};
+    if ((st = check_rows(gate, gate_stride, B, N, "gate", &ins[4])) != DFA_OK) return st;
+    const Region outs[] = {{Y, out, "Y"}};
+    if ((st = check_regions(outs, 1, ins, 5)) != DFA_OK) return st;
+    dfa::LinearLaunch a{};
+    a.X = X;
+    a.W = W;
+    a.bias = (const float*)bias;
+    a.gate = rows_of(gate, gate_stride);
+    a.residual = residual;
+    a.Y = Y;
+    a.act = act;
+    a.y_f32 = y_type == DFA_F32;
+    a.B = B;
+    a.L = L;
+    a.H = H;
+    a.K = K;
+    a.N = N;
+    return hip_status(dfa::launch_linear(a, stream), "linear launch");
+}
+
+dfa_status dfa_rope(const void* Q, const void* K, void* Qout, void* Kout, const void* pos, const int32_t* sections,
+                    int naxes, double base, int interleaved, int inverse, int B, int Hq, int Hk, int L, int d,
+                    int64_t pos_stride, hipStream_t stream) {
+    dfa_status st;
+    const bool both = K || Kout;
+    if (B <= 0 || Hq <= 0 || Hk < 0 || L <= 0 || d <= 0)
+        return fail(DFA_ERR_INVALID_ARG, "sizes must be positive (B=%d Hq=%d Hk=%d L=%d d=%d)", B, Hq, Hk, L, d);
+    if (both != (Hk > 0)) return fail(DFA_ERR_INVALID_ARG, "K and Kout must be given with Hk > 0 and only then (Hk=%d)", Hk);
+    if (d % 2 || d > dfa::ROPE_D_MAX)
+        return fail(DFA_ERR_UNSUPPORTED, "head dim d=%d is not built (even, at most %d)", d, dfa::ROPE_D_MAX);
+    if ((long long)B * L > (1LL << 30) || (long long)B * ((long long)Hq + Hk) > (1LL << 24) ||
+        (unsigned long long)B * L * ((unsigned long long)Hq + Hk) * d > (1ULL << 40))
+        return fail(DFA_ERR_INVALID_ARG, "tensors are too large (B=%d Hq=%d Hk=%d L=%d d=%d)", B, Hq, Hk, L, d);
+    if (naxes < 1 || naxes > dfa::ROPE_AXES_MAX)
+        return fail(DFA_ERR_INVALID_ARG, "naxes=%d must be 1 to %d", naxes, dfa::ROPE_AXES_MAX);
+    if (!sections) return fail(DFA_ERR_INVALID_ARG, "sections is NULL");
+    dfa::RopeLaunch a{};
+    long long sum = 0;
+    for (int i = 0; i < naxes; ++i) {
+        if (sections[i] < 2 || sections[i] % 2)
+            return fail(DFA_ERR_INVALID_ARG, "sections[%d]=%d must be even and at least 2", i, (int)sections[i]);
+        a.sections[i] = sections[i];
+        sum += sections[i];
+    }
+    if (sum > d) return fail(DFA_ERR_INVALID_ARG, "sections of %lld dims exceed d=%d", sum, d);
+    if (!(base > 0.0) || base > 1e300) return fail(DFA_ERR_INVALID_ARG, "base=%g must be positive and finite", base);
+    if (pos_stride < 0 || pos_stride > (1LL << 40) / B)
+        return fail(DFA_ERR_INVALID_ARG, "pos stride %lld is out of range", (long long)pos_stride);
+    if ((st = check_ptr(Q, "Q")) != DFA_OK) return st;
+    if ((st = check_ptr(Qout, "Qout")) != DFA_OK) return st;
+    if (both && (st = check_ptr(K, "K")) != DFA_OK) return st;
+    if (both && (st = check_ptr(Kout, "Kout")) != DFA_OK) return st;
+    if ((st = check_vector(pos, "pos", true)) != DFA_OK) return st;
+    const size_t row = (size_t)L * d * 2, qn = row * B * Hq, kn = row * B * Hk;
+    const Region Rq{Q, qn, "Q"}, Rk{K, kn, "K"}, Ro{Qout, qn, "Qout"}, Rko{Kout, kn, "Kout"},
+        Rp{pos, ((size_t)(B - 1) * (size_t)pos_stride + (size_t)L * naxes) * 4, "pos"};
+    const Region none{nullptr, 0, ""};
+    // an output against every tensor but the input that it may replace
+    const Region qins[] = {Qout == Q ? none : Rq, Rk, Rp}, kins[] = {Kout == K ? none : Rk, Rq, Rp};
+    const Region qouts[] = {Ro, Rko};
+    if ((st = check_regions(qouts, 2, nullptr, 0)) != DFA_OK) return st;
+    if ((st = check_regions(&Ro, 1, qins, 3)) != DFA_OK) return st;
+    if ((st = check_regions(&Rko, 1, kins, 3)) != DFA_OK) return st;
+    a.Q = Q;
+    a.K = K;
+    a.Qout = Qout;
+    a.Kout = Kout;
+    a.pos = (const float*)pos;
+    a.pos_stride = (long long)pos_stride;
+    a.naxes = naxes;
+    a.base = base;
+    a.interleaved = interleaved != 0;
+    a.inverse = inverse != 0;
+    a.B = B;
+    a.Hq = Hq;
+    a.Hk = Hk;
+    a.L = L;
+    a.d = d;
+    return hip_status(dfa::launch_rope(a, stream), "rotary positions launch");
+}
+
+// ---------------------------------------------------------------------------
 // Seeded plan generator
 // ---------------------------------------------------------------------------
 namespace {

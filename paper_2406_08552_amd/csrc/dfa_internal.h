@@ -35,6 +35,76 @@ struct ProjLaunch {
     int B, H, L, d;
 };
 
+// Rows of C fp32 values, one per batch entry `stride` elements apart (0: one
+// for all); p may be null.
+struct Rows {
+    const float* p;
+    long long stride;
+};
+
+// One layer norm launch over B * L tokens; x_f32: X (and dX) are fp32, else bf16.
+struct NormLaunch {
+    const void* X;
+    Rows weight, bias;
+    float offset, eps;
+    void* Y;
+    float* mean;
+    float* rstd;
+    bool x_f32;
+    int B, L, C;
+};
+struct NormGradLaunch {
+    const void* dY;
+    const void* X;
+    Rows weight;
+    float offset;
+    const float* mean;
+    const float* rstd;
+    void* dX;
+    float* dweight;
+    float* dbias;
+    float* partial;    // norm_grad_partials() values
+    bool x_f32;
+    int B, L, C, groups;
+};
+constexpr int NORM_C_MAX = 16384;
+constexpr int NORM_GROUPS_MAX = 1 << 22;   // a workgroup each at least
+hipError_t launch_layer_norm(const NormLaunch& a, hipStream_t stream);
+hipError_t launch_layer_norm_backward(const NormGradLaunch& a, hipStream_t stream);
+// fp32 values of workspace that the weight's and the bias's gradients take.
+size_t norm_grad_partials(int B, int L, int C, int groups);
+
+// One linear layer; act is a DFA_ACT_ code, y_f32: residual and Y are fp32, else bf16.
+struct LinearLaunch {
+    const void* X;
+    const void* W;
+    const float* bias;
+    Rows gate;
+    const void* residual;
+    void* Y;
+    int act;
+    bool y_f32;
+    int B, L, H, K, N;
+};
+hipError_t launch_linear(const LinearLaunch& a, hipStream_t stream);
+
+// One rotation of Q and K.
+constexpr int ROPE_D_MAX = 256, ROPE_AXES_MAX = 4;
+struct RopeLaunch {
+    const void* Q;
+    const void* K;
+    void* Qout;
+    void* Kout;
+    const float* pos;
+    long long pos_stride;
+    int sections[ROPE_AXES_MAX];
+    int naxes;
+    double base;
+    bool interleaved, inverse;
+    int B, Hq, Hk, L, d;
+};
+hipError_t launch_rope(const RopeLaunch& a, hipStream_t stream);
+
 hipError_t launch_mrae(const void* a, const void* b, size_t n, float eps, double* partial, int max_partials,
                        double* out, hipStream_t stream);
 // Workgroups (partial sums) of one MRAE reduction of n elements.

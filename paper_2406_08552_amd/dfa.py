@@ -30,10 +30,14 @@ CODE_NAMES = {FULL: "FULL", WARS_REFRESH: "WARS_REFRESH", WARS_REUSE: "WARS_REUS
               AST_REUSE: "AST_REUSE", ASC_REUSE: "ASC_REUSE",
               WARS_ASC_REFRESH: "WARS_ASC_REFRESH", WARS_ASC_REUSE: "WARS_ASC_REUSE"}
 
+BF16, F32 = 0, 1                                         # types of the residual stream
+ACT_NONE, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3   # activations of a linear layer
+
 # every symbol include/dfa.h declares
 EXPORTS = ("dfa_attn_full", "dfa_attn_full_and_residual", "dfa_attn_window_plus_residual",
            "dfa_plan_step", "dfa_plan_make", "dfa_qkv_proj", "dfa_out_proj", "dfa_module_step",
-           "dfa_mrae", "dfa_mrae_noalloc", "dfa_plan_search_workspace_bytes", "dfa_plan_search", "dfa_last_error", "dfa_version")
+           "dfa_mrae", "dfa_mrae_noalloc", "dfa_plan_search_workspace_bytes", "dfa_plan_search", "dfa_last_error", "dfa_version",
+           "dfa_layer_norm", "dfa_layer_norm_backward", "dfa_layer_norm_backward_workspace_bytes", "dfa_linear", "dfa_rope")
 MRAE_WORKSPACE_BYTES = 8192
 
 
@@ -82,6 +86,17 @@ def lib() -> ctypes.CDLL:
         L.dfa_plan_search.argtypes = [_int, _int, _vpp, _vpp, _vpp, _vpp, _vpp, ctypes.c_double] + [_int] * 5 + \
             [_vp, ctypes.c_size_t, _i32p, ctypes.POINTER(ctypes.c_double), _vp]
         L.dfa_plan_search.restype = _int
+        _i64, _f32 = ctypes.c_int64, ctypes.c_float
+        L.dfa_layer_norm.argtypes = [_vp] * 6 + [_int] * 4 + [_i64, _i64, _f32, _f32, _vp]
+        L.dfa_layer_norm.restype = _int
+        L.dfa_layer_norm_backward.argtypes = [_vp] * 9 + [ctypes.c_size_t] + [_int] * 4 + [_i64, _f32, _int, _vp]
+        L.dfa_layer_norm_backward.restype = _int
+        L.dfa_layer_norm_backward_workspace_bytes.argtypes = [_int] * 4
+        L.dfa_layer_norm_backward_workspace_bytes.restype = ctypes.c_size_t
+        L.dfa_linear.argtypes = [_vp] * 6 + [_int] * 7 + [_i64, _vp]
+        L.dfa_linear.restype = _int
+        L.dfa_rope.argtypes = [_vp] * 5 + [_i32p, _int, ctypes.c_double] + [_int] * 7 + [_i64, _vp]
+        L.dfa_rope.restype = _int
         L.dfa_last_error.argtypes = []
         L.dfa_last_error.restype = ctypes.c_char_p
         L.dfa_version.argtypes = []
@@ -293,6 +308,154 @@ def dfa_module_step(code: int, X, Wqkv, bqkv, Wo, bo, Q, K, V, O, R, Y, Ycache, 
     _weights(Wqkv, bqkv, Wo, bo, C)
     _check(lib().dfa_module_step(int(code), _ptr(X), _ptr(Wqkv), _ptr(bqkv), _ptr(Wo), _ptr(bo), _ptr(Q), _ptr(K),
                                  _ptr(V), _ptr(O), _ptr(R), _ptr(Y), _ptr(Ycache), B, H, L, d, w, _stream(stream)))
+
+
+def _same_device(*named):
+    """Every tensor on the current GPU: the kernels run there, on one of its streams."""
+    torch = _torch()
+    for t, name in named:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must live on a GPU (got {t.device})")
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _stream_type(t, name) -> int:
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise TypeError(f"{name}: expected bf16 or fp32, got {t.dtype}")
+
+
+def _rows(t, B, C, name) -> int:
+    """Elements between the batch entries' rows of an fp32 [C] or [B, C] tensor
+    whose rows are contiguous (0: one row for all)."""
+    if t is None:
+        return 0
+    if t.dtype != _torch().float32:
+        raise TypeError(f"{name}: expected fp32, got {t.dtype}")
+    if tuple(t.shape) not in ((C,), (B, C)) or (C > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: expected rows of {C} contiguous values, [{C}] or [{B}, {C}], got {tuple(t.shape)} "
+                         f"with strides {t.stride()}")
+    return t.stride(0) if t.dim() == 2 and B > 1 else 0
+
+
+def _tokens(t, name):
+    if t.dim() != 3:
+        raise ValueError(f"{name}: expected a [B, L, C] tensor, got {tuple(t.shape)}")
+    return tuple(t.shape)
+
+
+def dfa_layer_norm(X, weight, bias, Y, mean=None, rstd=None, eps: float = 1e-6, weight_offset: float = 0.0,
+                   stream=None) -> None:
+    """Y = (X - mean) * rstd * (weight + weight_offset) + bias over the last dim.
+    X [B, L, C] bf16 or fp32, Y [B, L, C] bf16; weight and bias fp32 [C], or
+    [B, C] rows that may be slices of a wider tensor, or None; mean and rstd
+    fp32 [B, L] outputs, or None.  weight_offset = 1 takes a modulation's scale."""
+    torch = _torch()
+    B, L, C = _tokens(X, "X")
+    xt = _stream_type(X, "X")
+    _same_device((X, "X"), (weight, "weight"), (bias, "bias"), (Y, "Y"), (mean, "mean"), (rstd, "rstd"))
+    _expect(X, X.dtype, (B, L, C), "X")
+    _expect(Y, torch.bfloat16, (B, L, C), "Y")
+    _expect(mean, torch.float32, (B, L), "mean")
+    _expect(rstd, torch.float32, (B, L), "rstd")
+    ws, bs = _rows(weight, B, C, "weight"), _rows(bias, B, C, "bias")
+    _check(lib().dfa_layer_norm(_ptr(X), _ptr(weight), _ptr(bias), _ptr(Y), _ptr(mean), _ptr(rstd), xt, B, L, C, ws, bs,
+                                weight_offset, eps, _stream(stream)))
+
+
+def layer_norm_backward_workspace_bytes(B: int, L: int, C: int, groups: int = 1) -> int:
+    """groups: rows of dweight and dbias, 1 or B."""
+    return int(lib().dfa_layer_norm_backward_workspace_bytes(B, L, C, groups))
+
+
+def dfa_layer_norm_backward(dY, X, weight, mean, rstd, dX, dweight, dbias, workspace=None, weight_offset: float = 0.0,
+                            stream=None) -> None:
+    """Gradients of dfa_layer_norm: dX [B, L, C] of X's type, dweight and dbias
+    fp32, each None, [C] (summed over the batch) or [B, C] (per batch entry; the
+    same for both).  workspace: a GPU tensor of at least
+    layer_norm_backward_workspace_bytes() bytes, where that is not 0."""
+    torch = _torch()
+    B, L, C = _tokens(X, "X")
+    xt = _stream_type(X, "X")
+    _same_device((dY, "dY"), (X, "X"), (weight, "weight"), (mean, "mean"), (rstd, "rstd"), (dX, "dX"),
+                 (dweight, "dweight"), (dbias, "dbias"), (workspace, "workspace"))
+    _expect(X, X.dtype, (B, L, C), "X")
+    _expect(dX, X.dtype, (B, L, C), "dX")
+    _expect(dY, torch.bfloat16, (B, L, C), "dY")
+    _expect(mean, torch.float32, (B, L), "mean")
+    _expect(rstd, torch.float32, (B, L), "rstd")
+    grads = [t for t in (dweight, dbias) if t is not None]
+    groups = B if grads and grads[0].dim() == 2 else 1
+    for t, name in ((dweight, "dweight"), (dbias, "dbias")):
+        _expect(t, torch.float32, (B, C) if grads and grads[0].dim() == 2 else (C,), name)
+    if workspace is not None:
+        _on_gpu((workspace, "workspace"))
+    ws = _rows(weight, B, C, "weight")
+    _check(lib().dfa_layer_norm_backward(_ptr(dY), _ptr(X), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dX), _ptr(dweight),
+                                         _ptr(dbias), _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
+                                         xt, B, L, C, ws, weight_offset, groups, _stream(stream)))
+
+
+def dfa_linear(X, W, bias, Y, act: int = ACT_NONE, gate=None, residual=None, stream=None) -> None:
+    """Y = residual + gate * act(X W^T + bias).  X bf16 [B, L, K], or the
+    attention output [B, H, L, d] read as its merged heads; W [N, K] bf16; bias
+    fp32 [N] or None; Y [B, L, N] bf16 or fp32; residual like Y (it may be Y) or
+    None; gate fp32 [N] or [B, N] rows, which may be slices, or None."""
+    torch = _torch()
+    if X.dim() == 4:
+        B, H, L, d = X.shape
+        K = H * d
+    else:
+        B, L, K = _tokens(X, "X")
+        H = 1
+    if Y.dim() != 3 or tuple(Y.shape[:2]) != (B, L):
+        raise ValueError(f"Y {tuple(Y.shape)} does not match [B, L, N] with B={B}, L={L}")
+    N = Y.shape[2]
+    yt = _stream_type(Y, "Y")
+    _same_device((X, "X"), (W, "W"), (bias, "bias"), (Y, "Y"), (gate, "gate"), (residual, "residual"))
+    _expect(X, torch.bfloat16, X.shape, "X")
+    _expect(W, torch.bfloat16, (N, K), "W")
+    _expect(bias, torch.float32, (N,), "bias")
+    _expect(Y, Y.dtype, (B, L, N), "Y")
+    _expect(residual, Y.dtype, (B, L, N), "residual")
+    gs = _rows(gate, B, N, "gate")
+    _check(lib().dfa_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), _ptr(Y), int(act), yt, B, L, H, K, N, gs,
+                            _stream(stream)))
+
+
+def dfa_rope(Q, K, Qout, Kout, pos, sections, base: float = 10000.0, interleaved: bool = False, inverse: bool = False,
+             stream=None) -> None:
+    """Rotates the pairs of Q [B, Hq, L, d] and K [B, Hk, L, d] (or None, with
+    Kout None) by their token's positions pos (fp32 [L, A], or [B, L, A]) along
+    the A axes, sections[a] dims of a head for axis a.  Outputs may be the
+    inputs.  interleaved: pairs (2i, 2i + 1) of a section instead of its halves;
+    inverse: the opposite rotation, which is also that of the gradients."""
+    torch = _torch()
+    if Q.dim() != 4:
+        raise ValueError(f"Q: expected a [B, H, L, d] tensor, got {tuple(Q.shape)}")
+    B, Hq, L, d = Q.shape
+    if (K is None) != (Kout is None):
+        raise ValueError("give K and Kout, or neither")
+    Hk = 0
+    if K is not None:
+        if K.dim() != 4 or (K.shape[0], K.shape[2], K.shape[3]) != (B, L, d):
+            raise ValueError(f"K {tuple(K.shape)} does not match Q {tuple(Q.shape)}")
+        Hk = K.shape[1]
+    _same_device((Q, "Q"), (K, "K"), (Qout, "Qout"), (Kout, "Kout"), (pos, "pos"))
+    for t, heads, name in ((Q, Hq, "Q"), (Qout, Hq, "Qout"), (K, Hk, "K"), (Kout, Hk, "Kout")):
+        _expect(t, torch.bfloat16, (B, heads, L, d), name)
+    A = len(sections)
+    _expect(pos, torch.float32, (B, L, A) if pos.dim() == 3 else (L, A), "pos")
+    stride = L * A if pos.dim() == 3 and B > 1 else 0
+    sec = (ctypes.c_int32 * max(A, 1))(*[int(n) for n in sections])
+    _check(lib().dfa_rope(_ptr(Q), _ptr(K), _ptr(Qout), _ptr(Kout), _ptr(pos), sec, A, float(base), int(bool(interleaved)),
+                          int(bool(inverse)), B, Hq, Hk, L, d, stride, _stream(stream)))
 
 
 def _on_gpu(*named):
