@@ -42,6 +42,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "dfa_epilogue.h"
 #include "dfa_internal.h"
 
 namespace dfa {
@@ -68,6 +69,7 @@ struct Tile {
     static constexpr int CPF = TF / 8 / NW;               // the first CPF of them feature rows
     static constexpr int SCRATCH = 32 * 32;               // scratch of a wavefront: one 32 x 32 block of output, or its biases
     static constexpr int STORES = 2 * MB * NB;            // stores of a wavefront's output, one destination
+    static constexpr int ROW_STORES = 16 * NB * (MB == 3 ? 2 : 1);   // of a linear layer's output, at least
     static_assert(TF % (8 * NW) == 0 && TT % (8 * NW) == 0 && NW % 2 == 0, "copies per wavefront");
     static_assert(8 * MB <= 64 && 64 * MB <= SCRATCH, "biases of a wavefront");
     static_assert((size_t)(NST * STAGE + NW * SCRATCH) * 2 * WGS <= 160 * 1024, "LDS");
@@ -87,7 +89,10 @@ __device__ __forceinline__ int swz(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int chunk_off(int row, int ch) { return row * GK + ((ch ^ swz(row)) << 3); }
 
 enum { ACT_ROWS = 0, ACT_HEADS = 1 };   // activations: [M][K] rows, or O [B][H][L][d]
-enum { OUT_QKV = 0, OUT_ROWS = 1 };     // epilogue: scatter to Q/K/V, or [M][N] rows
+enum { OUT_QKV = 0, OUT_ROWS = 1,       // epilogue: scatter to Q/K/V, or [M][N] rows,
+       OUT_LINEAR = 2,                  // or a linear layer's rows with its activation, gate and residual,
+       OUT_LINEAR_TAIL = 3 };           // where K is no multiple of 128
+constexpr bool is_linear(int out) { return out == OUT_LINEAR || out == OUT_LINEAR_TAIL; }
 
 struct GemmParams {
     const uint16_t* W;
@@ -101,7 +106,16 @@ struct GemmParams {
     uint32_t lmul, lshift, dmul, dshift;   // division by L and by d (fast_div)
     int group;               // token tiles per group of the block order (1: all feature tiles of a token tile in turn)
     int nblocks;
+    // OUT_LINEAR
+    Rows gate;
+    const void* residual;
+    void* Y;
+    int act_code;            // DFA_ACT_
+    bool y_f32;
 };
+
+// What lanes copy whose chunk lies behind the end of a row (OUT_LINEAR_TAIL).
+__device__ __attribute__((aligned(16))) uint32_t zero_chunk[4];
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
@@ -117,11 +131,21 @@ __device__ __forceinline__ void xchg32(uint32_t& a, uint32_t& b) {
 // m v - 2^(30 + s) < v <= 2^s, so n m >> (30 + s) is exact, and m <= 2^31.
 __device__ __forceinline__ int fast_div(int n, uint32_t mul, uint32_t shift) { return (int)((uint64_t)n * mul >> shift); }
 
+// Linear layers: the feature, within its workgroup's tile, whose weights row r
+// of a stage holds.  A wavefront's output has its features in lanes, so lane c
+// of its 32 gets neighbours to store together: 2c and 2c + 1 of the first 64,
+// and c of a third block of 32.
+template <class T>
+__device__ __forceinline__ int feature_of(int r) {
+    const int w = r / (32 * T::MB), q = r - w * (32 * T::MB), c = q & 31, mb = q >> 5;
+    return w * (32 * T::MB) + (T::MB >= 2 && mb < 2 ? 2 * c + mb : q);
+}
+
 // The copies of one wavefront: copy i fills the eight rows from
 // 8 (wave + i NW) of a stage, lane l the 16-byte slot l of them, with the
 // chunk that the swizzle places there: every row is one whole 128-byte line
 // of its operand.  Rows of one copy are all features or all tokens.
-template <int ACT, class T>
+template <int ACT, int OUT, class T>
 struct Copier {
     uint32_t off[T::CPW];        // byte offset of the lane's chunk from its operand's uniform base
     const char* wbase;           // the uniform bases: W's first feature row of the tile, at the next k-tile,
@@ -129,6 +153,7 @@ struct Copier {
     const char* ptr[ACT == ACT_HEADS ? T::CPW - T::CPF : 1];   // ACT_HEADS token rows: the lane's address
     int j;                       // ACT_HEADS: dim of the lane's chunk within its head
     int wave, lrow, ch;
+    int left;                    // OUT_LINEAR_TAIL: elements of a row from the lane's chunk of the next k-tile on
 
     __device__ __forceinline__ void init(int wave_, int lane) {
         wave = wave_;
@@ -142,11 +167,13 @@ struct Copier {
         wbase = (const char*)(p.W + (size_t)n0 * p.K);
         abase = ACT == ACT_ROWS ? (const char*)(p.act + (size_t)t0 * p.K) : nullptr;
         j = 8 * ch;                                     // < d: d is at least 64
+        left = p.K - 8 * ch;
 #pragma unroll
         for (int i = 0; i < T::CPW; ++i) {
             // rows beyond the last feature or token copy the last one (their outputs are not stored)
             if (i < T::CPF) {
-                const int row = (wave + i * T::NW) * 8 + lrow;
+                int row = (wave + i * T::NW) * 8 + lrow;
+                if constexpr (is_linear(OUT)) row = feature_of<T>(row);
                 off[i] = (uint32_t)min(row, p.N - 1 - n0) * (uint32_t)(2 * p.K) + 16u * ch;
             } else {
                 const int tr = min((wave + i * T::NW) * 8 + lrow - T::TF, p.M - 1 - t0);
@@ -166,6 +193,7 @@ struct Copier {
     __device__ __forceinline__ void park(const GemmParams& p) {
         wbase = (const char*)p.W;
         abase = (const char*)p.act;
+        left = p.K - 8 * ch;
 #pragma unroll
         for (int i = 0; i < T::CPW; ++i) off[i] = 16u * ch;
         if constexpr (ACT == ACT_HEADS) {
@@ -186,7 +214,10 @@ struct Copier {
         for (int i = 0; i < T::CPW; ++i) {
             __attribute__((address_space(3))) void* to =
                 (__attribute__((address_space(3))) void*)(st + (wave + i * T::NW) * 8 * GK);
-            if (i < T::CPF)
+            if constexpr (OUT == OUT_LINEAR_TAIL) {
+                const char* from = (i < T::CPF ? wbase : abase) + off[i];
+                __builtin_amdgcn_global_load_lds((const void*)(left > 0 ? from : (const char*)zero_chunk), to, 16, 0, 0);
+            } else if (i < T::CPF)
                 __builtin_amdgcn_global_load_lds((const void*)(wbase + off[i]), to, 16, 0, 0);
             else if constexpr (ACT == ACT_ROWS)
                 __builtin_amdgcn_global_load_lds((const void*)(abase + off[i]), to, 16, 0, 0);
@@ -194,6 +225,7 @@ struct Copier {
                 __builtin_amdgcn_global_load_lds((const void*)ptr[i - T::CPF], to, 16, 0, 0);
         }
         wbase += advance ? 2 * GK : 0;
+        left -= advance ? GK : 0;
         if constexpr (ACT == ACT_ROWS) {
             abase += advance ? 2 * GK : 0;
         } else {
@@ -230,13 +262,15 @@ struct Frag {
     }
 };
 
-// MFMAs [I0, I1) of the wavefront's MB x NB blocks.
-template <class T, int I0, int I1>
+// MFMAs [I0, I1) of the wavefront's MB x NB blocks: features x tokens, or
+// (LIN) tokens x features, whose lanes hold features.
+template <class T, bool LIN, int I0, int I1>
 __device__ __forceinline__ void mma(f32x16 (&acc)[T::MB][T::NB], const Frag<T>& f) {
 #pragma unroll
     for (int i = I0; i < I1; ++i) {
         const int mb = i / T::NB, nb = i % T::NB;
-        acc[mb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[mb], f.b[nb], acc[mb][nb], 0, 0, 0);
+        acc[mb][nb] = LIN ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b[nb], f.a[mb], acc[mb][nb], 0, 0, 0)
+                          : __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[mb], f.b[nb], acc[mb][nb], 0, 0, 0);
     }
 }
 
@@ -323,6 +357,85 @@ __device__ __forceinline__ void store_tile(const GemmParams& p, f32x16 (&acc)[T:
     }
 }
 
+// Output of one wavefront of a linear layer, straight from the accumulators:
+// lane c = lane % 32 holds the E features from f on of 16 tokens per block of
+// 32.  E = 2: whole 128-byte lines (fp32: 256 bytes) of a token leave at once.
+template <class T, bool WHOLE, bool F32, int E, int MB0>
+__device__ __forceinline__ void store_features(const GemmParams& p, f32x16 (&acc)[T::MB][T::NB], int f, int tw0, int lane) {
+    constexpr int SZ = F32 ? 4 : 2;
+    const int h = lane >> 5;
+    const int n = WHOLE ? E : min(E, p.N - f);   // features there
+    float g[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) g[e] = 1.f;
+    int entry = -1;
+    auto gate_of = [&](int t) {
+        const int en = p.gate.stride ? fast_div(t, p.lmul, p.lshift) : 0;
+        if (en == entry) return;
+        entry = en;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (WHOLE || e < n) g[e] = p.gate.p[(size_t)en * p.gate.stride + f + e];
+    };
+    const size_t base = ((size_t)tw0 * p.N + f) * SZ;
+    const char* res = (const char*)p.residual + base;
+    char* out = (char*)p.Y + base;
+    const uint32_t rowb = (uint32_t)p.N * SZ;
+#pragma unroll
+    for (int nb = 0; nb < T::NB; ++nb) {
+        float r[16][E];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int t = 32 * nb + 8 * (i / 4) + 4 * h + i % 4;
+#pragma unroll
+            for (int e = 0; e < E; ++e) r[i][e] = 0.f;
+            if (p.residual && (WHOLE || tw0 + t < p.M)) {
+                if (WHOLE || n == E) {
+                    read_row<F32, E>(r[i], res + t * rowb);
+                } else if (n > 0) {
+                    float one[1];
+                    read_row<F32, 1>(one, res + t * rowb);
+                    r[i][0] = one[0];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int t = 32 * nb + 8 * (i / 4) + 4 * h + i % 4;
+            if (!WHOLE && (tw0 + t >= p.M || n <= 0)) continue;
+            float z[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) z[e] = acc[MB0 + e][nb][i];
+            activate<E>(z, p.act_code);
+            if (p.gate.p) gate_of(tw0 + t);
+#pragma unroll
+            for (int e = 0; e < E; ++e) z[e] = fmaf(z[e], g[e], r[i][e]);
+            if (WHOLE || n == E) {
+                write_row<F32, E>(z, out + t * rowb);
+            } else {
+                float one[1] = {z[0]};
+                write_row<F32, 1>(one, out + t * rowb);
+            }
+        }
+    }
+}
+
+template <class T, bool WHOLE>
+__device__ __forceinline__ void store_linear(const GemmParams& p, f32x16 (&acc)[T::MB][T::NB], int nw0, int tw0, int lane) {
+    asm volatile("" : "+v"(lane));
+    const int c = lane & 31;
+    auto part = [&](auto e, auto mb0, int f) {
+        if (p.y_f32) store_features<T, WHOLE, true, decltype(e)::N, decltype(mb0)::N>(p, acc, f, tw0, lane);
+        else store_features<T, WHOLE, false, decltype(e)::N, decltype(mb0)::N>(p, acc, f, tw0, lane);
+    };
+    if constexpr (T::MB == 1) {
+        part(Left<1>{}, Left<0>{}, nw0 + c);
+    } else {
+        part(Left<2>{}, Left<0>{}, nw0 + 2 * c);
+        if constexpr (T::MB == 3) part(Left<1>{}, Left<2>{}, nw0 + 64 + c);
+    }
+}
+
 // First feature and token of tile b: groups of p.group token tiles, each
 // group's tiles feature tile by feature tile (a bijection; the last group may
 // be short).
@@ -338,11 +451,12 @@ template <int ACT, int OUT, class T>
 __global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(T::WGS * T::NW / 4, T::WGS * T::NW / 4)))
 gemm_stream_kernel(GemmParams p) {
     constexpr int MB = T::MB, NB = T::NB;
+    constexpr bool LIN = is_linear(OUT);
     // one array per stage: the compiler then knows that the copies into one
     // stage do not touch the stage being read, and adds no wait of its own
     __shared__ __attribute__((aligned(16))) uint16_t s0[T::STAGE];
     __shared__ __attribute__((aligned(16))) uint16_t s1[T::STAGE];
-    __shared__ __attribute__((aligned(16))) uint16_t scratch[T::NW * T::SCRATCH];
+    __shared__ __attribute__((aligned(16))) uint16_t scratch[LIN ? 8 : T::NW * T::SCRATCH];
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -359,13 +473,18 @@ gemm_stream_kernel(GemmParams p) {
     int n0, t0;
     tile_origin<T>(p, blk, n0, t0);
 
-    Copier<ACT, T> cp;
+    Copier<ACT, OUT, T> cp;
     cp.init(wave, lane);
-    const int nk = p.K / GK;                           // even
-    // the biases of the wavefront's features, four to a lane
+    const int nk = (p.K + 2 * GK - 1) / (2 * GK) * 2;   // even; OUT_LINEAR_TAIL: the last ones hold zeros
+    // the biases of the wavefront's features, four to a lane (linear layers: those of the lane's features)
     f32x4 bv{0.f, 0.f, 0.f, 0.f};
     auto load_bias = [&](int n) {
-        if (p.bias && lane < 8 * MB) bv = *(const f32x4*)(p.bias + min(n + 32 * MB * wf + 4 * lane, p.N - 4));
+        if constexpr (LIN) {
+            if (p.bias) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) bv[mb] = p.bias[min(n + feature_of<T>(32 * (MB * wf + mb) + r32), p.N - 1)];
+            }
+        } else if (p.bias && lane < 8 * MB) bv = *(const f32x4*)(p.bias + min(n + 32 * MB * wf + 4 * lane, p.N - 4));
     };
     uint16_t* sw = scratch + wave * T::SCRATCH;
     cp.start(p, n0, t0);
@@ -392,32 +511,32 @@ gemm_stream_kernel(GemmParams p) {
         // only wait out whole, so reads issued earlier would be waited for too
         constexpr int N = MB * NB, N0 = N > 2 ? 2 : 1;
         asm volatile("" : "+v"(ao), "+v"(bo));   // opaque: the reads' offsets are formed anew, not kept in registers
-        mma<T, 0, N0>(acc, f0);
+        mma<T, LIN, 0, N0>(acc, f0);
         __builtin_amdgcn_sched_barrier(0);
         f1.read(cur, 1, ao, bo);
         __builtin_amdgcn_sched_barrier(0);
-        mma<T, N0, N>(acc, f0);
-        mma<T, 0, N0>(acc, f1);
+        mma<T, LIN, N0, N>(acc, f0);
+        mma<T, LIN, 0, N0>(acc, f1);
         __builtin_amdgcn_sched_barrier(0);
         f0.read(cur, 2, ao, bo);
         __builtin_amdgcn_sched_barrier(0);
-        mma<T, N0, N>(acc, f1);
-        mma<T, 0, N0>(acc, f0);
+        mma<T, LIN, N0, N>(acc, f1);
+        mma<T, LIN, 0, N0>(acc, f0);
         __builtin_amdgcn_sched_barrier(0);
         f1.read(cur, 3, ao, bo);
         __builtin_amdgcn_sched_barrier(0);
-        mma<T, N0, N>(acc, f0);
+        mma<T, LIN, N0, N>(acc, f0);
         fence();
         // not __syncthreads(): its fence would wait for every copy and store
         __builtin_amdgcn_s_waitcnt(waitcnt(decltype(left)::N, true));
         __builtin_amdgcn_s_barrier();
         fence();
-        mma<T, 0, N0>(acc, f1);
+        mma<T, LIN, 0, N0>(acc, f1);
         __builtin_amdgcn_sched_barrier(0);
         then();
         if constexpr (decltype(left)::AHEAD) f0.read(nxt, 0, ao, bo);
         __builtin_amdgcn_sched_barrier(0);
-        mma<T, N0, N>(acc, f1);
+        mma<T, LIN, N0, N>(acc, f1);
         __builtin_amdgcn_sched_barrier(0);
     };
     // k-tiles 0 and 1 have landed
@@ -427,14 +546,23 @@ gemm_stream_kernel(GemmParams p) {
     fence();
     f0.read(s0, 0, ao, bo);
     while (true) {
-        init_acc<T>(acc, sw, bv, lane);
+        if constexpr (LIN) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[mb][nb][i] = bv[mb];
+        } else {
+            init_acc<T>(acc, sw, bv, lane);
+        }
         auto more0 = [&] { cp.issue(p, s0); };
         auto more1 = [&] { cp.issue(p, s1); };
         if (nk > 2) {
             // the T::STORES newest operations in flight may be stores of the
             // previous tile, issued behind this tile's first two k-tiles of
             // copies (if it had fewer, everything has been waited for)
-            step(Left<T::STORES>{}, s0, s1, more0);
+            step(Left<(LIN ? (T::ROW_STORES < 60 ? T::ROW_STORES : 60) : T::STORES)>{}, s0, s1, more0);
             step(Left<0>{}, s1, s0, more1);
         }
         for (int kt = 4; kt < nk; kt += 2) {
@@ -461,10 +589,12 @@ gemm_stream_kernel(GemmParams p) {
         });
         step(Left<0, false>{}, s1, s0, [&] { cp.issue(p, s1); });
         fence();
-        if (whole) {
-            store_tile<OUT, T, true>(p, acc, sw, nw0, tw0, lane);   // at least T::STORES stores
+        if (whole) {   // at least T::STORES (T::ROW_STORES) stores
+            if constexpr (LIN) store_linear<T, true>(p, acc, nw0, tw0, lane);
+            else store_tile<OUT, T, true>(p, acc, sw, nw0, tw0, lane);
         } else {
-            store_tile<OUT, T, false>(p, acc, sw, nw0, tw0, lane);
+            if constexpr (LIN) store_linear<T, false>(p, acc, nw0, tw0, lane);
+            else store_tile<OUT, T, false>(p, acc, sw, nw0, tw0, lane);
             __builtin_amdgcn_s_waitcnt(waitcnt(0, true));
         }
         fence();
@@ -481,11 +611,12 @@ template <int ACT, int OUT, class T>
 __global__ void __launch_bounds__(T::NT) __attribute__((amdgpu_waves_per_eu(T::WGS * T::NW / 4, T::WGS * T::NW / 4)))
 gemm_ring_kernel(GemmParams p) {
     static_assert(T::NST == 4, "stages");
+    constexpr bool LIN = is_linear(OUT);
     __shared__ __attribute__((aligned(16))) uint16_t s0[T::STAGE];
     __shared__ __attribute__((aligned(16))) uint16_t s1[T::STAGE];
     __shared__ __attribute__((aligned(16))) uint16_t s2[T::STAGE];
     __shared__ __attribute__((aligned(16))) uint16_t s3[T::STAGE];
-    __shared__ __attribute__((aligned(16))) uint16_t scratch[T::NW * T::SCRATCH];
+    __shared__ __attribute__((aligned(16))) uint16_t scratch[LIN ? 8 : T::NW * T::SCRATCH];
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -495,9 +626,9 @@ gemm_ring_kernel(GemmParams p) {
     int n0, t0;
     tile_origin<T>(p, x * q + min(x, rem) + ((int)blockIdx.x >> 3), n0, t0);
 
-    Copier<ACT, T> cp;
+    Copier<ACT, OUT, T> cp;
     cp.init(wave, lane);
-    const int nk = p.K / GK;                           // even
+    const int nk = (p.K + 2 * GK - 1) / (2 * GK) * 2;   // even
     f32x4 bv[T::MB][4];
 #pragma unroll
     for (int mb = 0; mb < T::MB; ++mb)
@@ -507,8 +638,14 @@ gemm_ring_kernel(GemmParams p) {
 #pragma unroll
         for (int mb = 0; mb < T::MB; ++mb)
 #pragma unroll
-            for (int jb = 0; jb < 4; ++jb)
-                bv[mb][jb] = *(const f32x4*)(p.bias + min(n0 + 32 * (T::MB * wf + mb) + 8 * jb + 4 * h, p.N - 4));
+            for (int jb = 0; jb < 4; ++jb) {
+                if constexpr (LIN) {
+                    const float b = p.bias[min(n0 + feature_of<T>(32 * (T::MB * wf + mb) + r32), p.N - 1)];
+                    bv[mb][jb] = f32x4{b, b, b, b};
+                } else {
+                    bv[mb][jb] = *(const f32x4*)(p.bias + min(n0 + 32 * (T::MB * wf + mb) + 8 * jb + 4 * h, p.N - 4));
+                }
+            }
     }
     cp.start(p, n0, t0);
     // every k-tile issues the same number of copies: behind the last one its
@@ -545,7 +682,7 @@ gemm_ring_kernel(GemmParams p) {
         for (int ks = 0; ks < 4; ++ks) nf[ks].read(nxt, ks, ao, bo);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) mma<T, 0, T::MB * T::NB>(acc, cf[ks]);
+        for (int ks = 0; ks < 4; ++ks) mma<T, LIN, 0, T::MB * T::NB>(acc, cf[ks]);
         __builtin_amdgcn_sched_barrier(0);
     };
     fence();
@@ -567,8 +704,14 @@ gemm_ring_kernel(GemmParams p) {
     }
     uint16_t* sw = scratch + wave * T::SCRATCH;
     const int nw0 = n0 + 32 * T::MB * wf, tw0 = t0 + 32 * T::NB * wt;
-    if (n0 + T::TF <= p.N && t0 + T::TT <= p.M) store_tile<OUT, T, true>(p, acc, sw, nw0, tw0, lane);
-    else store_tile<OUT, T, false>(p, acc, sw, nw0, tw0, lane);
+    const bool whole = n0 + T::TF <= p.N && t0 + T::TT <= p.M;
+    if constexpr (LIN) {
+        if (whole) store_linear<T, true>(p, acc, nw0, tw0, lane);
+        else store_linear<T, false>(p, acc, nw0, tw0, lane);
+    } else {
+        if (whole) store_tile<OUT, T, true>(p, acc, sw, nw0, tw0, lane);
+        else store_tile<OUT, T, false>(p, acc, sw, nw0, tw0, lane);
+    }
     // no copy may land after this workgroup's LDS is given to another
     __builtin_amdgcn_s_waitcnt(waitcnt(0, true));
 }
@@ -591,10 +734,10 @@ hipError_t launch_shape(GemmParams& p, hipStream_t stream) {
     fast_divisor(p.d, p.dmul, p.dshift);
     if constexpr (T::NST > 2) {
         hipLaunchKernelGGL((gemm_ring_kernel<ACT, OUT, T>), dim3(p.nblocks), dim3(T::NT), 0, stream, p);
-        return hipGetLastError();
+    } else {
+        const int grid = (int)(nb < 256 * T::WGS ? nb : 256 * T::WGS);
+        hipLaunchKernelGGL((gemm_stream_kernel<ACT, OUT, T>), dim3(grid), dim3(T::NT), 0, stream, p);
     }
-    const int grid = (int)(nb < 256 * T::WGS ? nb : 256 * T::WGS);
-    hipLaunchKernelGGL((gemm_stream_kernel<ACT, OUT, T>), dim3(grid), dim3(T::NT), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -656,6 +799,27 @@ hipError_t launch_qkv_proj(const ProjLaunch& a, hipStream_t stream) {
     p.K = a.H * a.d;
     p.N = 3 * p.K;
     return launch_gemm<ACT_ROWS, OUT_QKV>(p, stream);
+}
+
+// K % 8 = 0 (rows are 16-byte aligned), and K % 128 = 0 for merged heads.
+hipError_t launch_linear_tiles(const LinearLaunch& a, hipStream_t stream) {
+    GemmParams p{};
+    p.W = (const uint16_t*)a.W;
+    p.act = (const uint16_t*)a.X;
+    p.bias = a.bias;
+    p.L = a.L;
+    p.H = a.H;
+    p.d = a.K / a.H;
+    p.M = a.B * a.L;
+    p.K = a.K;
+    p.N = a.N;
+    p.gate = a.gate;
+    p.residual = a.residual;
+    p.Y = a.Y;
+    p.act_code = a.act;
+    p.y_f32 = a.y_f32;
+    if (a.H > 1) return launch_gemm<ACT_HEADS, OUT_LINEAR>(p, stream);
+    return a.K % (2 * GK) ? launch_gemm<ACT_ROWS, OUT_LINEAR_TAIL>(p, stream) : launch_gemm<ACT_ROWS, OUT_LINEAR>(p, stream);
 }
 
 hipError_t launch_out_proj(const ProjLaunch& a, hipStream_t stream) {

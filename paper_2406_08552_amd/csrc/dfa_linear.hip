@@ -3,7 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "dfa.h"
+#include "dfa_epilogue.h"
 #include "dfa_internal.h"
 
 namespace dfa {
@@ -24,19 +24,6 @@ struct LinearParams {
     int M, N, K, L, H, d;      // d = K / H
     int nft, ntt;              // feature and token tiles
 };
-
-__device__ __forceinline__ float activate(float z, int act) {
-    switch (act) {
-        case DFA_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        case DFA_ACT_GELU_TANH: {
-            // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u))
-            const float u = 1.5957691216057308f * (z + 0.044715f * z * z * z);
-            return z / (1.f + __expf(-u));
-        }
-        case DFA_ACT_SILU: return z / (1.f + __expf(-z));
-        default: return z;
-    }
-}
 
 // Eight consecutive k of a row at p, of which n are there (n >= 8: all), zeros behind.
 __device__ __forceinline__ u32x4 load8(const uint16_t* p, int n) {
@@ -66,10 +53,12 @@ __global__ void __launch_bounds__(256) linear_general_kernel(LinearParams p) {
     if (p.H == 1) xr += (size_t)t * p.K;
     else xr += ((size_t)b * p.H * p.L + (t - b * p.L)) * p.d;
     const uint16_t* wr = p.W + (size_t)min(n0 + row, p.N - 1) * p.K;
+    const int wt = wave & 1, wf = wave >> 1;
+    const int f = n0 + 32 * wf + r32;
+    const float bias = p.bias ? p.bias[min(f, p.N - 1)] : 0.f;
     f32x16 acc;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-    const int wt = wave & 1, wf = wave >> 1;
+    for (int i = 0; i < 16; ++i) acc[i] = bias;
     for (int k0 = 0; k0 < p.K; k0 += 32) {
         const int k = k0 + ch;
         u32x4 xv{0, 0, 0, 0}, wv{0, 0, 0, 0};
@@ -90,29 +79,24 @@ __global__ void __launch_bounds__(256) linear_general_kernel(LinearParams p) {
             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w, acc, 0, 0, 0);
         }
     }
-    const int f = n0 + 32 * wf + r32;
     if (f >= p.N) return;
-    const float bias = p.bias ? p.bias[f] : 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int tt = t0 + 32 * wt + 8 * (i / 4) + 4 * h + i % 4;
         if (tt >= p.M) continue;
-        float z = activate(acc[i] + bias, p.act);
-        if (p.gate.p) z *= p.gate.p[(size_t)(tt / p.L) * p.gate.stride + f];
-        const size_t o = (size_t)tt * p.N + f;
-        if constexpr (YF32) {
-            if (p.residual) z += ((const float*)p.residual)[o];
-            ((float*)p.Y)[o] = z;
-        } else {
-            if (p.residual) z += __builtin_bit_cast(float, (uint32_t)((const uint16_t*)p.residual)[o] << 16);
-            ((uint16_t*)p.Y)[o] = __builtin_bit_cast(uint16_t, (__bf16)z);
-        }
+        float z[1] = {acc[i]}, r[1] = {0.f};
+        const size_t o = ((size_t)tt * p.N + f) * (YF32 ? 4 : 2);
+        if (p.residual) read_row<YF32, 1>(r, (const char*)p.residual + o);
+        activate<1>(z, p.act);
+        z[0] = fmaf(z[0], p.gate.p ? p.gate.p[(size_t)(tt / p.L) * p.gate.stride + f] : 1.f, r[0]);
+        write_row<YF32, 1>(z, (char*)p.Y + o);
     }
 }
 
 }  // namespace
 
 hipError_t launch_linear(const LinearLaunch& a, hipStream_t stream) {
+    if (a.K % (a.H > 1 ? 128 : 8) == 0) return launch_linear_tiles(a, stream);
     LinearParams p{};
     p.X = (const uint16_t*)a.X;
     p.W = (const uint16_t*)a.W;
