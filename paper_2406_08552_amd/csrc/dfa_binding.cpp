@@ -24,6 +24,14 @@ typedef int (*out_fn)(const void*, const void*, const void*, void*, int, int, in
 typedef int (*module_fn)(int, const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*,
                          void*, void*, void*, int, int, int, int, int, stream_t);
 typedef int (*mrae_fn)(const void*, const void*, size_t, void*, double*, stream_t);
+typedef int (*norm_fn)(const void*, const void*, const void*, void*, void*, void*, int, int, int, int, int64_t, int64_t, float,
+                       float, stream_t);
+typedef int (*norm_grad_fn)(const void*, const void*, const void*, const void*, const void*, void*, void*, void*, void*, size_t,
+                            int, int, int, int, int64_t, float, int, stream_t);
+typedef int (*linear_fn)(const void*, const void*, const void*, const void*, const void*, void*, int, int, int, int, int, int,
+                         int, int64_t, stream_t);
+typedef int (*rope_fn)(const void*, const void*, void*, void*, const void*, const int32_t*, int, double, int, int, int, int, int,
+                       int, int, int64_t, stream_t);
 
 struct Functions {
     attn_fn attn[3];      // full, full_and_residual, window_plus_residual
@@ -32,6 +40,10 @@ struct Functions {
     out_fn out;
     module_fn module;
     mrae_fn mrae;
+    norm_fn norm;
+    norm_grad_fn norm_grad;
+    linear_fn linear;
+    rope_fn rope;
     PyObject* device;       // torch's current device, and
     PyObject* raw_stream;   // its current stream of a device, as integers
 };
@@ -102,6 +114,71 @@ struct Reader {
             ok = false;
         }
         return p;
+    }
+};
+
+// Arguments of the block's operators: their tensors are on the current device.
+struct BlockReader : Reader {
+    stream_t st = nullptr;
+    int64_t device = -1;
+
+    explicit BlockReader(const Functions& f) {
+        PyObject* dev = f.norm ? PyObject_CallNoArgs(f.device) : nullptr;   // not bound: nothing is ordinary
+        PyObject* s = dev ? PyObject_CallOneArg(f.raw_stream, dev) : nullptr;
+        device = dev ? PyLong_AsLongLong(dev) : -1;
+        st = s ? PyLong_AsVoidPtr(s) : nullptr;
+        ok = dev && s;
+        Py_XDECREF(dev);
+        Py_XDECREF(s);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            ok = false;
+        }
+    }
+    const at::Tensor* here(PyObject* o) {
+        const at::Tensor* t = tensor(o);
+        ok = ok && t->is_cuda() && t->get_device() == device;
+        return ok ? t : nullptr;
+    }
+    // address of a contiguous tensor of this type and shape (None: null, where it may be)
+    void* at_shape(PyObject* o, at::ScalarType type, at::IntArrayRef shape, bool optional = false) {
+        if (!ok || (optional && o == Py_None)) return nullptr;
+        const at::Tensor* t = here(o);
+        ok = ok && t->scalar_type() == type && t->sizes() == shape && t->is_contiguous();
+        return ok ? t->data_ptr() : nullptr;
+    }
+    // rows of C fp32 values, [C] or [B][C] with any distance between rows
+    void* rows(PyObject* o, int64_t B, int64_t C, int64_t& stride) {
+        stride = 0;
+        if (!ok || o == Py_None) return nullptr;
+        const at::Tensor* t = here(o);
+        if (!ok) return nullptr;
+        const at::IntArrayRef n = t->sizes();
+        const bool each = n.size() == 2;
+        ok = t->scalar_type() == F32 && (each ? n[0] == B && n[1] == C : n.size() == 1 && n[0] == C) &&
+             (C <= 1 || t->strides()[each ? 1 : 0] == 1);
+        if (!ok) return nullptr;
+        stride = each && B > 1 ? t->strides()[0] : 0;
+        return t->data_ptr();
+    }
+    // 0: bf16, 1: fp32
+    int stream_type(const at::Tensor* t) {
+        ok = ok && (t->scalar_type() == BF16 || t->scalar_type() == F32);
+        return ok && t->scalar_type() == F32;
+    }
+    double number(PyObject* o) {
+        ok = ok && (PyFloat_CheckExact(o) || PyLong_CheckExact(o));
+        if (!ok) return 0;
+        const double v = PyFloat_AsDouble(o);
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            ok = false;
+        }
+        return v;
+    }
+    int truth(PyObject* o) {
+        ok = ok && PyBool_Check(o);
+        return ok && o == Py_True;
     }
 };
 
@@ -239,6 +316,152 @@ PyObject* py_mrae(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// As guarded(), for the block's operators.
+template <class F>
+PyObject* guarded_block(Py_ssize_t n, Py_ssize_t want, F&& read) {
+    if (n != want) return PyLong_FromLong(-1);
+    BlockReader r(g_functions);
+    int status = -1;
+    try {
+        if (r.ok) status = read(r, g_functions);
+    } catch (...) {
+        r.ok = false;
+    }
+    return PyLong_FromLong(r.ok ? status : -1);
+}
+
+// layer_norm(X, weight, bias, Y, mean, rstd, eps, weight_offset)
+PyObject* py_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded_block(n, 8, [&](BlockReader& r, const Functions& f) -> int {
+        const at::Tensor* x = r.here(a[0]);
+        r.ok = r.ok && x->sizes().size() == 3;
+        if (!r.ok) return -1;
+        const at::IntArrayRef s = x->sizes();
+        const int type = r.stream_type(x), B = r.dim(s[0]), L = r.dim(s[1]), C = r.dim(s[2]);
+        const int64_t tokens[2] = {B, L};
+        int64_t ws, bs;
+        void *X = r.at_shape(a[0], x->scalar_type(), s), *w = r.rows(a[1], B, C, ws), *b = r.rows(a[2], B, C, bs),
+             *Y = r.at_shape(a[3], BF16, s), *mean = r.at_shape(a[4], F32, tokens, true), *rstd = r.at_shape(a[5], F32, tokens, true);
+        const float eps = (float)r.number(a[6]), off = (float)r.number(a[7]);
+        return call(r, [&] { return f.norm(X, w, b, Y, mean, rstd, type, B, L, C, ws, bs, off, eps, r.st); });
+    });
+}
+
+// layer_norm_backward(dY, X, weight, mean, rstd, dX, dweight, dbias, workspace, weight_offset)
+PyObject* py_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded_block(n, 10, [&](BlockReader& r, const Functions& f) -> int {
+        const at::Tensor* x = r.here(a[1]);
+        r.ok = r.ok && x->sizes().size() == 3;
+        if (!r.ok) return -1;
+        const at::IntArrayRef s = x->sizes();
+        const int type = r.stream_type(x), B = r.dim(s[0]), L = r.dim(s[1]), C = r.dim(s[2]);
+        const at::Tensor* grad = a[6] != Py_None ? r.here(a[6]) : a[7] != Py_None ? r.here(a[7]) : nullptr;
+        if (!r.ok) return -1;
+        const bool each = grad && grad->sizes().size() == 2;
+        const int64_t tokens[2] = {B, L}, one[1] = {C}, all[2] = {B, C};
+        const at::IntArrayRef sums = each ? at::IntArrayRef(all) : at::IntArrayRef(one);
+        int64_t ws;
+        void *dY = r.at_shape(a[0], BF16, s), *X = r.at_shape(a[1], x->scalar_type(), s), *w = r.rows(a[2], B, C, ws),
+             *mean = r.at_shape(a[3], F32, tokens), *rstd = r.at_shape(a[4], F32, tokens),
+             *dX = r.at_shape(a[5], x->scalar_type(), s), *dw = r.at_shape(a[6], F32, sums, true),
+             *db = r.at_shape(a[7], F32, sums, true), *space = nullptr;
+        size_t bytes = 0;
+        if (r.ok && a[8] != Py_None) {
+            const at::Tensor* t = r.here(a[8]);
+            r.ok = r.ok && t->is_contiguous();
+            if (!r.ok) return -1;
+            space = t->data_ptr();
+            bytes = (size_t)t->numel() * t->element_size();
+        }
+        const float off = (float)r.number(a[9]);
+        const int groups = each ? B : 1;
+        return call(r, [&] {
+            return f.norm_grad(dY, X, w, mean, rstd, dX, dw, db, space, bytes, type, B, L, C, ws, off, groups, r.st);
+        });
+    });
+}
+
+// linear(X, W, bias, Y, act, gate, residual)
+PyObject* py_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded_block(n, 7, [&](BlockReader& r, const Functions& f) -> int {
+        const at::Tensor* x = r.here(a[0]);
+        const at::Tensor* y = r.here(a[3]);
+        r.ok = r.ok && (x->sizes().size() == 3 || x->sizes().size() == 4) && y->sizes().size() == 3;
+        if (!r.ok) return -1;
+        const at::IntArrayRef xs = x->sizes(), ys = y->sizes();
+        const bool heads = xs.size() == 4;
+        const int type = r.stream_type(y), B = r.dim(xs[0]), H = heads ? r.dim(xs[1]) : 1, L = r.dim(xs[heads ? 2 : 1]);
+        const int64_t width = heads ? xs[1] * xs[3] : xs[2];   // each at most 2^31 (dim)
+        r.ok = r.ok && (!heads || xs[3] <= INT_MAX) && ys[0] == B && ys[1] == L;
+        const int K = r.dim(width), N = r.dim(ys[2]), act = r.integer(a[4]);
+        const int64_t w[2] = {N, K}, b[1] = {N};
+        int64_t gs;
+        void *X = r.at_shape(a[0], BF16, xs), *W = r.at_shape(a[1], BF16, w), *bias = r.at_shape(a[2], F32, b, true),
+             *Y = r.at_shape(a[3], y->scalar_type(), ys), *gate = r.rows(a[5], B, N, gs),
+             *res = r.at_shape(a[6], y->scalar_type(), ys, true);
+        return call(r, [&] { return f.linear(X, W, bias, gate, res, Y, act, type, B, L, H, K, N, gs, r.st); });
+    });
+}
+
+// rope(Q, K, Qout, Kout, pos, sections, base, interleaved, inverse)
+PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded_block(n, 9, [&](BlockReader& r, const Functions& f) -> int {
+        const Heads q(r, a[0]);
+        r.ok = r.ok && (a[1] == Py_None) == (a[3] == Py_None) && (PyList_CheckExact(a[5]) || PyTuple_CheckExact(a[5]));
+        if (!r.ok) return -1;
+        int Hk = 0;
+        at::IntArrayRef ks;
+        if (a[1] != Py_None) {
+            const Heads k(r, a[1]);
+            r.ok = r.ok && k.B == q.B && k.L == q.L && k.d == q.d;
+            ks = k.shape;
+            Hk = k.H;
+        }
+        const Py_ssize_t axes = PySequence_Fast_GET_SIZE(a[5]);
+        int32_t sections[8];
+        r.ok = r.ok && axes <= 8;
+        for (Py_ssize_t i = 0; r.ok && i < axes; ++i) sections[i] = r.integer(PySequence_Fast_GET_ITEM(a[5], i));
+        const at::Tensor* p = r.here(a[4]);
+        if (!r.ok) return -1;
+        const bool each = p->sizes().size() == 3;
+        const int64_t one[2] = {q.L, axes}, all[3] = {q.B, q.L, axes};
+        const int64_t stride = each && q.B > 1 ? q.L * (int64_t)axes : 0;
+        void *Q = r.at_shape(a[0], BF16, q.shape), *K = r.at_shape(a[1], BF16, ks, true), *Qo = r.at_shape(a[2], BF16, q.shape),
+             *Ko = r.at_shape(a[3], BF16, ks, true),
+             *pos = r.at_shape(a[4], F32, each ? at::IntArrayRef(all) : at::IntArrayRef(one));
+        const double base = r.number(a[6]);
+        const int inter = r.truth(a[7]), inverse = r.truth(a[8]);
+        return call(r, [&] {
+            return f.rope(Q, K, Qo, Ko, pos, sections, (int)axes, base, inter, inverse, q.B, q.H, Hk, q.L, q.d, stride, r.st);
+        });
+    });
+}
+
+// init_block(layer_norm, layer_norm_backward, linear, rope): the functions' addresses
+PyObject* py_init_block(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 4) {
+        PyErr_SetString(PyExc_TypeError, "init_block takes 4 arguments");
+        return nullptr;
+    }
+    void* p[4];
+    for (int i = 0; i < 4; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null function address");
+            return nullptr;
+        }
+    }
+    if (!g_functions.device) {
+        PyErr_SetString(PyExc_ValueError, "init comes first");
+        return nullptr;
+    }
+    g_functions.norm = (norm_fn)p[0];
+    g_functions.norm_grad = (norm_grad_fn)p[1];
+    g_functions.linear = (linear_fn)p[2];
+    g_functions.rope = (rope_fn)p[3];
+    Py_RETURN_NONE;
+}
+
 // init(device, raw_stream, full, full_and_residual, window, plan, qkv, out, module, mrae): the functions' addresses
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 10) {
@@ -272,7 +495,9 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef g_methods[] = {
     DFA_METHOD("init", py_init), DFA_METHOD("attn", py_attn),     DFA_METHOD("plan_step", py_plan),
     DFA_METHOD("qkv_proj", py_qkv), DFA_METHOD("out_proj", py_out), DFA_METHOD("module_step", py_module),
-    DFA_METHOD("mrae", py_mrae), {nullptr, nullptr, 0, nullptr}};
+    DFA_METHOD("mrae", py_mrae), DFA_METHOD("init_block", py_init_block), DFA_METHOD("layer_norm", py_norm),
+    DFA_METHOD("layer_norm_backward", py_norm_grad), DFA_METHOD("linear", py_linear), DFA_METHOD("rope", py_rope),
+    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_dfa_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -22,8 +22,10 @@ __device__ __forceinline__ void activate(float (&z)[E], int act) {
             z[e] = fmaf(half, erff(x * 0.70710678118654752f), half);
         } else {
             // (1 + tanh(u)) / 2 = 1 / (1 + exp(-2 u)), u = sqrt(2 / pi) (x + 0.044715 x^3)
-            const float u = act == DFA_ACT_SILU ? x : 1.5957691216057308f * fmaf(0.044715f * x * x, x, x);
-            z[e] = x / (1.f + __expf(-u));
+            // the exponential in base 2; v_rcp_f32 is within one unit of the last place, where a division takes ten instructions
+            const float u = act == DFA_ACT_SILU ? -1.4426950408889634f * x
+                                                : x * fmaf(-0.10294324f, x * x, -2.3022082f);
+            z[e] = x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u));
         }
     }
 }

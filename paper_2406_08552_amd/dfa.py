@@ -133,6 +133,8 @@ def _native():
                  "dfa_qkv_proj", "dfa_out_proj", "dfa_module_step", "dfa_mrae")
         mod.init(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
                  *[ctypes.cast(getattr(L, n), _vp).value for n in names])
+        mod.init_block(*[ctypes.cast(getattr(L, n), _vp).value
+                         for n in ("dfa_layer_norm", "dfa_layer_norm_backward", "dfa_linear", "dfa_rope")])
         _NATIVE = mod
     return _NATIVE
 
@@ -356,6 +358,8 @@ def dfa_layer_norm(X, weight, bias, Y, mean=None, rstd=None, eps: float = 1e-6, 
     X [B, L, C] bf16 or fp32, Y [B, L, C] bf16; weight and bias fp32 [C], or
     [B, C] rows that may be slices of a wider tensor, or None; mean and rstd
     fp32 [B, L] outputs, or None.  weight_offset = 1 takes a modulation's scale."""
+    if stream is None and _done(_native().layer_norm(X, weight, bias, Y, mean, rstd, eps, weight_offset)):
+        return
     torch = _torch()
     B, L, C = _tokens(X, "X")
     xt = _stream_type(X, "X")
@@ -380,6 +384,9 @@ def dfa_layer_norm_backward(dY, X, weight, mean, rstd, dX, dweight, dbias, works
     fp32, each None, [C] (summed over the batch) or [B, C] (per batch entry; the
     same for both).  workspace: a GPU tensor of at least
     layer_norm_backward_workspace_bytes() bytes, where that is not 0."""
+    if stream is None and _done(_native().layer_norm_backward(dY, X, weight, mean, rstd, dX, dweight, dbias, workspace,
+                                                              weight_offset)):
+        return
     torch = _torch()
     B, L, C = _tokens(X, "X")
     xt = _stream_type(X, "X")
@@ -407,6 +414,8 @@ def dfa_linear(X, W, bias, Y, act: int = ACT_NONE, gate=None, residual=None, str
     attention output [B, H, L, d] read as its merged heads; W [N, K] bf16; bias
     fp32 [N] or None; Y [B, L, N] bf16 or fp32; residual like Y (it may be Y) or
     None; gate fp32 [N] or [B, N] rows, which may be slices, or None."""
+    if stream is None and _done(_native().linear(X, W, bias, Y, act, gate, residual)):
+        return
     torch = _torch()
     if X.dim() == 4:
         B, H, L, d = X.shape
@@ -436,6 +445,8 @@ def dfa_rope(Q, K, Qout, Kout, pos, sections, base: float = 10000.0, interleaved
     the A axes, sections[a] dims of a head for axis a.  Outputs may be the
     inputs.  interleaved: pairs (2i, 2i + 1) of a section instead of its halves;
     inverse: the opposite rotation, which is also that of the gradients."""
+    if stream is None and _done(_native().rope(Q, K, Qout, Kout, pos, sections, base, interleaved, inverse)):
+        return
     torch = _torch()
     if Q.dim() != 4:
         raise ValueError(f"Q: expected a [B, H, L, d] tensor, got {tuple(Q.shape)}")
