@@ -31,18 +31,21 @@ __device__ __forceinline__ void activate(float (&z)[E], int act) {
 }
 
 // E neighbouring values of a row of Y or of the residual, at the alignment of
-// one element (rows of any width).
+// one element (rows of any width; the hardware takes global accesses at any).
 template <bool F32, int E>
 __device__ __forceinline__ void read_row(float (&x)[E], const char* p) {
     if constexpr (F32) {
         __builtin_memcpy(x, p, 4 * E);
-    } else if constexpr (E == 2) {
-        uint32_t u;
-        __builtin_memcpy(&u, p, 4);
-        x[0] = __builtin_bit_cast(float, u << 16);
-        x[1] = __builtin_bit_cast(float, u & 0xFFFF0000u);
+    } else if constexpr (E % 2 == 0) {
+        uint32_t u[E / 2];
+        __builtin_memcpy(u, p, 2 * E);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            x[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+            x[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xFFFF0000u);
+        }
     } else {
-        static_assert(E == 1, "one or two");
+        static_assert(E == 1, "one, or an even number");
         x[0] = __builtin_bit_cast(float, (uint32_t) * (const uint16_t*)p << 16);
     }
 }
@@ -51,11 +54,13 @@ __device__ __forceinline__ void write_row(const float (&x)[E], char* p) {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     if constexpr (F32) {
         __builtin_memcpy(p, x, 4 * E);
-    } else if constexpr (E == 2) {
-        const uint32_t u = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[0], (__bf16)x[1]});
-        __builtin_memcpy(p, &u, 4);
+    } else if constexpr (E % 2 == 0) {
+        uint32_t u[E / 2];
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) u[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
+        __builtin_memcpy(p, u, 2 * E);
     } else {
-        static_assert(E == 1, "one or two");
+        static_assert(E == 1, "one, or an even number");
         *(uint16_t*)p = __builtin_bit_cast(uint16_t, (__bf16)x[0]);
     }
 }

@@ -87,7 +87,6 @@ struct LinearLaunch {
     int B, L, H, K, N;
 };
 hipError_t launch_linear(const LinearLaunch& a, hipStream_t stream);
-hipError_t launch_linear_tiles(const LinearLaunch& a, hipStream_t stream);
 
 // One rotation of Q and K.
 constexpr int ROPE_D_MAX = 256, ROPE_AXES_MAX = 4;
