@@ -2,11 +2,13 @@
 // turns by theta = pos[token][axis] base^(-2 i / n), to
 // (x cos - y sin, x sin + y cos); the inverse turns by -theta.
 //
-// An HBM stream of Q and K.  A lane owns some pairs of one token (so that an
+// An HBM stream of Q and K.  A lane owns some dims of one token (so that an
 // output may replace its input) and walks the heads with them: their angles
 // are formed once for all heads of Q and K that the lane visits.  The angle is
 // reduced in fp64, in revolutions, because a position of thousands times a
-// frequency near 1 leaves fp32 few bits of the fraction.
+// frequency near 1 leaves fp32 few bits of the fraction; sine and cosine of
+// the fraction are v_sin_f32 and v_cos_f32, off by at most 1.25e-7 over 2^22
+// fractions of -1/2 to 1/2.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -16,8 +18,11 @@
 namespace dfa {
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int BATCH = 4;        // heads whose loads a lane has in flight
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int BATCH = 4;       // heads whose loads a lane has in flight
 constexpr uint8_t KEEP = 255;   // "axis" of the dims behind the last section
 
 struct RopeParams {
@@ -31,49 +36,202 @@ struct RopeParams {
     int units;               // lanes per token
     int tokens;              // per workgroup
     int per_block;           // heads that one workgroup visits
-    float sign;
-    double freq[ROPE_D_MAX / 2];    // per pair: base^(-2 i / n) / (2 pi)
-    uint8_t axis[ROPE_D_MAX / 2];   // and its axis, or KEEP
-    uint8_t lo[ROPE_D_MAX / 2];     // per unit of halves: first dim of its first elements,
-    uint8_t hi[ROPE_D_MAX / 2];     // and of their partners
+    int sections[ROPE_AXES_MAX];   // 0 behind the last
+    double log2_base;
+    bool interleaved, inverse;
 };
 
 __device__ __forceinline__ float bf16_at(uint16_t x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
 __device__ __forceinline__ uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 
-// U pairs per lane: INTER, 2 U consecutive elements; else U at lo and U at hi.
+// What a head's dims turn by, formed by the workgroup (a lane per dim: a table
+// among the kernel's arguments, read by every wavefront, took longer): a dim
+// becomes x cos(phi) + partner sin(phi) with phi = pos[axis] * 2 pi turn, where
+// turn is -base^(-2 i / n) / (2 pi) for the first of a pair, + for the second.
+struct Dims {
+    double turn[ROPE_D_MAX];
+    uint8_t axis[ROPE_D_MAX], partner[ROPE_D_MAX];
+    uint8_t lo[ROPE_D_MAX / 2];    // halves: the first of the pairs, in order
+    __device__ __forceinline__ void form(const RopeParams& p) {
+        static_assert(THREADS >= ROPE_D_MAX, "a lane per dim");
+        const int x = threadIdx.x;
+        if (x < p.d) {
+            // the section of x; the dims behind the last are one that does not turn
+            int o = 0, n = 0, s = KEEP, at = 0;
+#pragma unroll
+            for (int a = 0; a < ROPE_AXES_MAX; ++a) {
+                if (x >= at && x < at + p.sections[a]) {
+                    o = at;
+                    n = p.sections[a];
+                    s = a;
+                }
+                at += p.sections[a];
+            }
+            if (s == KEEP) {
+                o = at;
+                n = p.d - at;
+            }
+            const int i = x - o, half = n / 2;
+            const bool first = p.interleaved ? i % 2 == 0 : i < half;
+            const int pair = p.interleaved ? i / 2 : first ? i : i - half;
+            // 1 / (2 pi) turns per radian
+            const double t = s == KEEP ? 0.0 : 0.15915494309189533577 * exp2(-p.log2_base * (double)pair / (double)half);
+            turn[x] = first != p.inverse ? -t : t;
+            axis[x] = (uint8_t)s;
+            partner[x] = (uint8_t)(p.interleaved ? x ^ 1 : first ? x + half : x - half);
+            if (first) lo[o / 2 + pair] = (uint8_t)x;
+        }
+        __syncthreads();
+    }
+};
+
+// Positions of token l, and cosine and sine of one dim's angle.
+struct Angles {
+    float pos[ROPE_AXES_MAX];
+    __device__ __forceinline__ Angles(const RopeParams& p, int b, long long l) {
+        const float* at = p.pos + (size_t)b * p.pos_stride + (size_t)l * p.naxes;
+#pragma unroll
+        for (int a = 0; a < ROPE_AXES_MAX; ++a) pos[a] = a < p.naxes ? at[a] : 0.f;
+    }
+    __device__ __forceinline__ void of(double turn, int axis, float& c, float& s) const {
+        const float x = axis == 0 ? pos[0] : axis == 1 ? pos[1] : axis == 2 ? pos[2] : pos[3];
+        const double rev = (double)x * turn;
+        const float f = (float)(rev - rint(rev));
+        s = __builtin_amdgcn_sinf(f);
+        c = __builtin_amdgcn_cosf(f);
+    }
+};
+
+// Offset, in elements, of the row of head h (Q's heads, then K's) of token l.
+__device__ __forceinline__ size_t row_of(const RopeParams& p, int b, int h, long long l, int& which) {
+    which = h >= p.heads[0];
+    return (((size_t)b * p.heads[which] + (which ? h - p.heads[0] : h)) * p.L + l) * p.d;
+}
+
+enum { PAIRS, HALVES_EVEN, HALVES };   // partners: beside each other; pairs of dims in the other half; any dim
+
+// d % 8 = 0: a lane owns eight neighbouring dims, 16 bytes.  Halves: their
+// partners come from other lanes of the wavefront through LDS, by fours or (odd
+// halves) by twos of bytes; loads of a unit's own two parts, 4 bytes each at
+// d = 72 in sections of 36, took 76 us where this takes 67 (302 MB moved).
+template <int EX>
+__global__ void __launch_bounds__(THREADS) rope_rows_kernel(RopeParams p) {
+    __shared__ u32x4 xch[EX == PAIRS ? 1 : WAVES][EX == PAIRS ? 1 : BATCH][64];
+    __shared__ Dims dims;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int per_wave = p.tokens / WAVES;
+    const int lt = lane / p.units, d0 = 8 * (lane - lt * p.units);
+    const bool mine = lt < per_wave;
+    const int nh = p.heads[0] + p.heads[1];
+    const int h0 = blockIdx.y * p.per_block, h1 = min(nh, h0 + p.per_block);
+    bool formed = false;
+    double turn[8];
+    int axis[8], from[8];   // from: byte offset of the partner in the wavefront's rows
+    for (int b = blockIdx.z; b < p.B; b += gridDim.z)
+        // every wavefront of the workgroup makes the same number of rounds
+        for (long long t0 = (long long)blockIdx.x * p.tokens; t0 < p.L; t0 += (long long)gridDim.x * p.tokens) {
+            const long long l = t0 + wave * per_wave + lt;
+            const bool in = mine && l < p.L;
+            u32x4 next[BATCH];
+            auto load = [&](int h) {
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j)
+                    if (in && h + j < h1) {
+                        int which;
+                        const size_t row = row_of(p, b, h + j, l, which);
+                        next[j] = *(const u32x4*)(p.in[which] + 2 * (row + d0));
+                    }
+            };
+            // in flight while the turns are formed: the positions, and the first heads
+            const Angles ang(p, b, in ? l : t0);
+            load(h0);
+            if (!formed) {
+                formed = true;
+                dims.form(p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    turn[i] = dims.turn[d0 + i];
+                    axis[i] = dims.axis[d0 + i];
+                    from[i] = 2 * (lt * p.d + (axis[i] == KEEP ? d0 + i : dims.partner[d0 + i]));
+                }
+            }
+            float cs[8], sn[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (EX == PAIRS && i % 2) {   // the second of a pair turns by the same angle
+                    cs[i] = cs[i - 1];
+                    sn[i] = -sn[i - 1];
+                } else {
+                    ang.of(turn[i], axis[i], cs[i], sn[i]);
+                }
+            }
+            for (int h = h0; h < h1; h += BATCH) {
+                u32x4 x[BATCH];
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) x[j] = next[j];
+                if (h + BATCH < h1) load(h + BATCH);
+                if constexpr (EX != PAIRS) {
+#pragma unroll
+                    for (int j = 0; j < BATCH; ++j) xch[wave][j][lane] = x[j];
+                    __builtin_amdgcn_wave_barrier();   // the wavefront's LDS accesses complete in order
+                }
+#pragma unroll
+                for (int j = 0; j < BATCH; ++j) {
+                    if (!in || h + j >= h1) continue;
+                    const char* rows = (const char*)xch[EX == PAIRS ? 0 : wave][EX == PAIRS ? 0 : j];
+                    u32x4 y;
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        const uint32_t u = x[j][i / 2];
+                        uint32_t q;
+                        if constexpr (EX == PAIRS) q = u << 16 | u >> 16;
+                        else if constexpr (EX == HALVES_EVEN) q = *(const uint32_t*)(rows + from[i]);
+                        else q = *(const uint16_t*)(rows + from[i]) | (uint32_t) * (const uint16_t*)(rows + from[i + 1]) << 16;
+                        const float a = fmaf(bf16_at((uint16_t)u), cs[i], bf16_at((uint16_t)q) * sn[i]);
+                        const float c = fmaf(bf16_at(u >> 16), cs[i + 1], bf16_at(q >> 16) * sn[i + 1]);
+                        const uint32_t r = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)c});
+                        y[i / 2] = (axis[i] == KEEP ? u & 0xFFFFu : r & 0xFFFFu) | (axis[i + 1] == KEEP ? u & 0xFFFF0000u : r & 0xFFFF0000u);
+                    }
+                    int which;
+                    const size_t row = row_of(p, b, h + j, l, which);
+                    *(u32x4*)(p.out[which] + 2 * (row + d0)) = y;
+                }
+                if constexpr (EX != PAIRS) __builtin_amdgcn_wave_barrier();
+            }
+        }
+}
+
+// Other head dims: U pairs per lane.  INTER: 2 U consecutive elements; else U at lo and U at their partners.
 template <bool INTER, int U>
-__global__ void __launch_bounds__(THREADS) rope_kernel(RopeParams p) {
+__global__ void __launch_bounds__(THREADS) rope_units_kernel(RopeParams p) {
+    __shared__ Dims dims;
+    dims.form(p);
     const int lt = threadIdx.x / p.units, u = threadIdx.x - lt * p.units;
     if (lt >= p.tokens) return;
-    const int lo = INTER ? 2 * U * u : p.lo[u], hi = INTER ? lo + U : p.hi[u];
+    const int lo = INTER ? 2 * U * u : dims.lo[U * u], hi = INTER ? lo + U : dims.partner[lo];
     const int nh = p.heads[0] + p.heads[1];
     const int h0 = blockIdx.y * p.per_block, h1 = min(nh, h0 + p.per_block);
     for (int b = blockIdx.z; b < p.B; b += gridDim.z)
         for (long long l = (long long)blockIdx.x * p.tokens + lt; l < p.L; l += (long long)gridDim.x * p.tokens) {
             float cs[U], sn[U];
             bool keep[U];
+            const Angles ang(p, b, l);
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int a = p.axis[u * U + i];
-                keep[i] = a == KEEP;
-                const float pos = keep[i] ? 0.f : p.pos[(size_t)b * p.pos_stride + (size_t)l * p.naxes + a];
-                const double rev = (double)pos * p.freq[u * U + i];
-                sincospif(2.f * (float)(rev - rint(rev)), &sn[i], &cs[i]);
-                sn[i] *= p.sign;
+                const int first = lo + (INTER ? 2 * i : i);
+                keep[i] = dims.axis[first] == KEEP;
+                ang.of(dims.turn[first], dims.axis[first], cs[i], sn[i]);
             }
             for (int h = h0; h < h1; h += BATCH) {
                 uint16_t x[BATCH][2 * U];
-                size_t at[BATCH];
 #pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    const int which = h + j >= p.heads[0], hw = which ? h + j - p.heads[0] : h + j;
-                    at[j] = (((size_t)b * p.heads[which] + hw) * p.L + l) * p.d * 2;
+                for (int j = 0; j < BATCH; ++j)
                     if (h + j < h1) {
-                        __builtin_memcpy(x[j], p.in[which] + at[j] + 2 * lo, 2 * U);
-                        __builtin_memcpy(x[j] + U, p.in[which] + at[j] + 2 * hi, 2 * U);
+                        int which;
+                        const size_t row = row_of(p, b, h + j, l, which);
+                        __builtin_memcpy(x[j], p.in[which] + 2 * (row + lo), 2 * U);
+                        __builtin_memcpy(x[j] + U, p.in[which] + 2 * (row + hi), 2 * U);
                     }
-                }
 #pragma unroll
                 for (int j = 0; j < BATCH; ++j) {
                     if (h + j >= h1) break;
@@ -81,32 +239,48 @@ __global__ void __launch_bounds__(THREADS) rope_kernel(RopeParams p) {
                     for (int i = 0; i < U; ++i) {
                         uint16_t &s = x[j][INTER ? 2 * i : i], &t = x[j][INTER ? 2 * i + 1 : U + i];
                         const float xs = bf16_at(s), xt = bf16_at(t);
-                        const uint16_t ys = to_bf16(xs * cs[i] - xt * sn[i]), yt = to_bf16(xs * sn[i] + xt * cs[i]);
+                        const uint16_t ys = to_bf16(fmaf(xs, cs[i], xt * sn[i])), yt = to_bf16(fmaf(xt, cs[i], -(xs * sn[i])));
                         s = keep[i] ? s : ys;
                         t = keep[i] ? t : yt;
                     }
-                    char* out = p.out[h + j >= p.heads[0]] + at[j];
-                    __builtin_memcpy(out + 2 * lo, x[j], 2 * U);
-                    __builtin_memcpy(out + 2 * hi, x[j] + U, 2 * U);
+                    int which;
+                    const size_t row = row_of(p, b, h + j, l, which);
+                    __builtin_memcpy(p.out[which] + 2 * (row + lo), x[j], 2 * U);
+                    __builtin_memcpy(p.out[which] + 2 * (row + hi), x[j] + U, 2 * U);
                 }
             }
         }
 }
 
-template <bool INTER, int U>
-hipError_t run(RopeParams& p, hipStream_t stream) {
-    p.units = p.d / (2 * U);
-    p.tokens = THREADS / p.units;
+// Grid of a kernel whose workgroups take p.tokens tokens.
+dim3 grid_of(RopeParams& p) {
     const int nh = p.heads[0] + p.heads[1];
     const long long tiles = ((long long)p.L + p.tokens - 1) / p.tokens;
     // few workgroups: fewer heads each, down to one batch of loads
-    long long parts = (2048 + tiles * p.B - 1) / (tiles * p.B);
+    long long parts = (2047 + tiles * p.B) / (tiles * p.B);
     if (parts > (nh + BATCH - 1) / BATCH) parts = (nh + BATCH - 1) / BATCH;
     if (parts > 65535) parts = 65535;
     p.per_block = (int)((nh + parts - 1) / parts);
+    p.per_block = (p.per_block + BATCH - 1) / BATCH * BATCH;
     parts = (nh + p.per_block - 1) / p.per_block;
-    const unsigned gx = (unsigned)(tiles < (1 << 22) ? tiles : (1 << 22)), gz = p.B < 65535 ? p.B : 65535;
-    hipLaunchKernelGGL((rope_kernel<INTER, U>), dim3(gx, (unsigned)parts, gz), dim3(THREADS), 0, stream, p);
+    return dim3((unsigned)(tiles < (1 << 22) ? tiles : (1 << 22)), (unsigned)parts, p.B < 65535 ? p.B : 65535);
+}
+
+template <int EX>
+hipError_t run_rows(RopeParams& p, hipStream_t stream) {
+    p.units = p.d / 8;
+    p.tokens = WAVES * (64 / p.units);
+    const dim3 grid = grid_of(p);
+    hipLaunchKernelGGL((rope_rows_kernel<EX>), grid, dim3(THREADS), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <bool INTER, int U>
+hipError_t run_units(RopeParams& p, hipStream_t stream) {
+    p.units = p.d / (2 * U);
+    p.tokens = THREADS / p.units;
+    const dim3 grid = grid_of(p);
+    hipLaunchKernelGGL((rope_units_kernel<INTER, U>), grid, dim3(THREADS), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -126,41 +300,24 @@ hipError_t launch_rope(const RopeLaunch& a, hipStream_t stream) {
     p.B = a.B;
     p.L = a.L;
     p.d = a.d;
-    p.sign = a.inverse ? -1.f : 1.f;
-    // The pairs of every section in turn, then those of the dims that stay; one
-    // power per axis, the frequencies by multiplication.  U pairs go to a lane:
-    // as many (a 16-byte access at most) as divide every section's halves, or
-    // the head's pairs where they lie side by side.
-    int U = a.interleaved ? 4 : 8, n = 0, o = 0;
-    uint8_t first[ROPE_D_MAX / 2], partner[ROPE_D_MAX / 2];
-    for (int s = 0; s <= a.naxes; ++s) {
-        const int half = (s < a.naxes ? a.sections[s] : a.d - o) / 2;
-        const double ratio = s < a.naxes ? pow(a.base, -1.0 / half) : 0.0;
-        double f = s < a.naxes ? 0.15915494309189533577 : 0.0;   // 1 / (2 pi)
-        for (int i = 0; i < half; ++i, ++n) {
-            p.freq[n] = f;
-            p.axis[n] = s < a.naxes ? (uint8_t)s : KEEP;
-            first[n] = (uint8_t)(o + i);
-            partner[n] = (uint8_t)(o + half + i);
-            f *= ratio;
-        }
-        o += 2 * half;
-        while (!a.interleaved && half % U) U /= 2;
+    p.log2_base = log2(a.base);
+    p.interleaved = a.interleaved;
+    p.inverse = a.inverse;
+    bool even = true;   // every half a whole number of two dims
+    int rest = a.d;
+    for (int i = 0; i < a.naxes; ++i) {
+        p.sections[i] = a.sections[i];
+        even = even && a.sections[i] % 4 == 0;
+        rest -= a.sections[i];
     }
-    while (n % U) U /= 2;
-    for (int u = 0; u * U < n; ++u) {
-        p.lo[u] = first[u * U];
-        p.hi[u] = partner[u * U];
+    if (a.d % 8 == 0) {
+        if (a.interleaved) return run_rows<PAIRS>(p, stream);
+        return even ? run_rows<HALVES_EVEN>(p, stream) : run_rows<HALVES>(p, stream);
     }
-    if (a.interleaved) {
-        if (U == 4) return run<true, 4>(p, stream);
-        if (U == 2) return run<true, 2>(p, stream);
-        return run<true, 1>(p, stream);
-    }
-    if (U == 8) return run<false, 8>(p, stream);
-    if (U == 4) return run<false, 4>(p, stream);
-    if (U == 2) return run<false, 2>(p, stream);
-    return run<false, 1>(p, stream);
+    // two pairs to a lane where that divides the head's pairs (halves: every section's, and the rest's)
+    const int U = a.d % 4 == 0 && (a.interleaved || (even && rest % 4 == 0)) ? 2 : 1;
+    if (a.interleaved) return U == 2 ? run_units<true, 2>(p, stream) : run_units<true, 1>(p, stream);
+    return U == 2 ? run_units<false, 2>(p, stream) : run_units<false, 1>(p, stream);
 }
 
 }  // namespace dfa
