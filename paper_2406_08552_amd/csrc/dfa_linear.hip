@@ -29,7 +29,7 @@ struct LinearOut {
     static constexpr bool FROM_BIAS = false;
     static constexpr int E = F32 ? 4 : 8, SZ = F32 ? 4 : 2;        // features of a lane, bytes of an element
     static constexpr int RPI = 2 * E, REPS = 32 / RPI;             // tokens per instruction, instructions per block
-    static constexpr int BLOCKS = T::MB * T::NB, DEPTH = BLOCKS < 5 ? BLOCKS : 3;
+    static constexpr int BLOCKS = T::MB * T::NB, DEPTH = BLOCKS < 5 ? BLOCKS : BLOCKS < 8 ? 3 : 2;
     static_assert(T::STORES <= BLOCKS * REPS, "stores of a wavefront's output");
     u32x4 r[DEPTH][REPS];
 
@@ -152,99 +152,222 @@ __device__ __forceinline__ u32x4 load8(const uint16_t* p, int n) {
     return v;
 }
 
-// 64 features x 64 tokens per workgroup of four wavefronts, k by 32.
-template <bool YF32>
-__global__ void __launch_bounds__(256) linear_general_kernel(LinearParams p) {
-    constexpr int PITCH = 40;   // elements of an LDS row
-    __shared__ __attribute__((aligned(16))) uint16_t sx[64 * PITCH], sw[64 * PITCH];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, h = lane >> 5;
-    const int t0 = (blockIdx.x / p.nft) * 64, n0 = (blockIdx.x % p.nft) * 64;
-    const int row = tid >> 2, ch = (tid & 3) * 8;
-    const int t = min(t0 + row, p.M - 1);
-    const uint16_t* xr = p.act;
-    const int b = t / p.L;
-    if (p.H == 1) xr += (size_t)t * p.K;
-    else xr += ((size_t)b * p.H * p.L + (t - b * p.L)) * p.d;
-    const uint16_t* wr = p.W + (size_t)min(n0 + row, p.N - 1) * p.K;
-    const int wt = wave & 1, wf = wave >> 1;
-    const int f = n0 + 32 * wf + r32;
-    const float bias = p.bias ? p.bias[min(f, p.N - 1)] : 0.f;
-    f32x16 acc;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-    for (int k0 = 0; k0 < p.K; k0 += 32) {
-        const int k = k0 + ch;
-        u32x4 xv{0, 0, 0, 0}, wv{0, 0, 0, 0};
-        if (k < p.K) {
-            // heads: a chunk of eight lies in one head (d % 8 = 0)
-            const uint16_t* at = p.H == 1 ? xr + k : xr + (size_t)(k / p.d) * p.L * p.d + k % p.d;
-            xv = load8(at, p.K - k);
-            wv = load8(wr + k, p.K - k);
-        }
-        __syncthreads();
-        *(u32x4*)(sx + row * PITCH + ch) = xv;
-        *(u32x4*)(sw + row * PITCH + ch) = wv;
-        __syncthreads();
-#pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const bf16x8 a = __builtin_bit_cast(bf16x8, *(const u32x4*)(sx + (32 * wt + r32) * PITCH + 16 * ks + 8 * h));
-            const bf16x8 w = __builtin_bit_cast(bf16x8, *(const u32x4*)(sw + (32 * wf + r32) * PITCH + 16 * ks + 8 * h));
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w, acc, 0, 0, 0);
+// Element k of token t of the activations, k a multiple of 8 (heads: a chunk of
+// eight lies in one, since d % 8 = 0).
+struct TokenRow {
+    const uint16_t* p;
+    long long head;   // elements from a head's dims on to the next head's, less d
+    __device__ __forceinline__ TokenRow(const LinearParams& q, int t) {
+        if (q.H == 1) {
+            p = q.act + (size_t)t * q.K;
+            head = 0;
+        } else {
+            const int b = fast_div(t, q.lmul, q.lshift);
+            p = q.act + ((size_t)t + (size_t)b * (q.H - 1) * q.L) * q.d;
+            head = (long long)(q.L - 1) * q.d;
         }
     }
-    if (f >= p.N) return;
+    __device__ __forceinline__ const uint16_t* at(const LinearParams& q, int k) const {
+        return head ? p + k + fast_div(k, q.dmul, q.dshift) * head : p + k;
+    }
+};
+
+// Any K: rows that 16 bytes do not divide take no direct copies, so the k-tiles pass through registers, the next one in
+// flight while this one is multiplied.
+template <bool F32, class T>
+__global__ void __launch_bounds__(T::NT) linear_any_kernel(LinearParams p) {
+    constexpr int CH = (T::TF + T::TT) * 8 / T::NT;   // chunks of eight k per lane and k-tile
+    using Out = LinearOut<F32, T>;
+    __shared__ __attribute__((aligned(16))) uint16_t st[2][T::STAGE];
+    __shared__ __attribute__((aligned(16))) uint16_t scratch[T::NW * Out::SCRATCH];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wf = wave % T::WF, wt = wave / T::WF, r32 = lane & 31, h = lane >> 5;
+    int n0, t0;
+    const int x = blockIdx.x & 7, q = p.nblocks >> 3, rem = p.nblocks & 7;
+    tile_origin<T>(p, x * q + min(x, rem) + ((int)blockIdx.x >> 3), n0, t0);
+    const int row = tid >> 3, ch = tid & 7;           // and the rows NT / 8 apart
+    u32x4 v[CH];
+    auto load = [&](int k0) {
+        const int k = k0 + 8 * ch;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int tt = t0 + 32 * wt + 8 * (i / 4) + 4 * h + i % 4;
-        if (tt >= p.M) continue;
-        float z[1] = {acc[i] + bias}, r[1] = {0.f};
-        const size_t o = ((size_t)tt * p.N + f) * (YF32 ? 4 : 2);
-        if (p.residual) read_row<YF32, 1>(r, (const char*)p.residual + o);
+        for (int i = 0; i < CH; ++i) {
+            const int r = row + i * (T::NT / 8);
+            v[i] = u32x4{0, 0, 0, 0};
+            if (k < p.K) {
+                const uint16_t* from = r < T::TF ? p.W + (size_t)min(n0 + r, p.N - 1) * p.K + k
+                                                 : p.act + (size_t)min(t0 + r - T::TF, p.M - 1) * p.K + k;
+                v[i] = load8(from, p.K - k);
+            }
+        }
+    };
+    f32x16 acc[T::MB][T::NB];
+    zero_acc<T>(acc);
+    const int ao = chunk_off(32 * T::MB * wf + r32, h), bo = chunk_off(T::TF + 32 * T::NB * wt + r32, h);
+    load(0);
+    const int nk = (p.K + GK - 1) / GK;
+    for (int kt = 0; kt < nk; ++kt) {
+        uint16_t* cur = st[kt & 1];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) *(u32x4*)(cur + chunk_off(row + i * (T::NT / 8), ch)) = v[i];
+        __syncthreads();   // behind it every wavefront has read the k-tile before this one
+        if (kt + 1 < nk) load((kt + 1) * GK);
+        Frag<T> f;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            f.read(cur, ks, ao, bo);
+            mma<T, 0, T::MB * T::NB>(acc, f);
+        }
+    }
+    const bool whole = n0 + T::TF <= p.N && t0 + T::TT <= p.M;
+    const int nw0 = n0 + 32 * T::MB * wf, tw0 = t0 + 32 * T::NB * wt;
+    Out out;
+    out.ahead(p, nw0, tw0, lane, whole);
+    if (whole) out.template store<true>(p, acc, scratch + wave * Out::SCRATCH, nw0, tw0, lane);
+    else out.template store<false>(p, acc, scratch + wave * Out::SCRATCH, nw0, tw0, lane);
+}
+
+// Few tokens (at most 16 TB): the weights' stream from HBM counts.  A workgroup
+// takes 16 features; its wavefronts take the 64-element pieces of K in turn,
+// straight into registers (16 features x 128 bytes, AHEAD pieces in flight),
+// through v_mfma_f32_16x16x32_bf16 (A element e = A[l % 16][8 (l / 16) + e], B
+// alike, output element i = D[4 (l / 16) + i][l % 16]), and add up in LDS.
+template <bool F32, int TB>
+__global__ void __launch_bounds__(512) linear_few_kernel(LinearParams p) {
+    constexpr int NW = 8, AHEAD = TB > 1 ? 2 : 3;
+    __shared__ float sums[NW][TB][16][17];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, kq = 8 * (lane >> 4), n0 = 16 * blockIdx.x;
+    const uint16_t* w = p.W + (size_t)min(n0 + r, p.N - 1) * p.K;
+    f32x4 acc[TB];
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb) acc[tb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    u32x4 wv[AHEAD][2], xv[AHEAD][2][TB];
+    auto load = [&](int slot, int k0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int k = k0 + 32 * i + kq;
+            wv[slot][i] = u32x4{0, 0, 0, 0};
+            if (k < p.K) wv[slot][i] = load8(w + k, p.K - k);
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb) {
+                xv[slot][i][tb] = u32x4{0, 0, 0, 0};
+                if (k < p.K) xv[slot][i][tb] = load8(TokenRow(p, min(16 * tb + r, p.M - 1)).at(p, k), p.K - k);
+            }
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) load(s, (wave + s * NW) * 64);
+    for (int k0 = wave * 64; k0 < p.K; k0 += AHEAD * NW * 64) {
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) {   // pieces behind the end are zeros
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int tb = 0; tb < TB; ++tb)
+                    acc[tb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[s][i][tb]),
+                                                                      __builtin_bit_cast(bf16x8, wv[s][i]), acc[tb], 0, 0, 0);
+            load(s, k0 + (AHEAD + s) * NW * 64);
+        }
+    }
+#pragma unroll
+    for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[wave][tb][4 * (lane >> 4) + i][r] = acc[tb][i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < TB * 256; e += 512) {
+        const int t = e >> 4, f = n0 + (e & 15);
+        if (t >= p.M || f >= p.N) continue;
+        float z[1] = {0.f}, x[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < NW; ++i) z[0] += sums[i][t >> 4][t & 15][e & 15];
+        if (p.bias) z[0] += p.bias[f];
+        const size_t o = ((size_t)t * p.N + f) * (F32 ? 4 : 2);
+        if (p.residual) read_row<F32, 1>(x, (const char*)p.residual + o);
         activate<1>(z, p.act_code);
-        z[0] = fmaf(z[0], p.gate.p ? p.gate.p[(size_t)(tt / p.L) * p.gate.stride + f] : 1.f, r[0]);
-        write_row<YF32, 1>(z, (char*)p.Y + o);
+        const float g = p.gate.p ? p.gate.p[(size_t)fast_div(t, p.lmul, p.lshift) * p.gate.stride + f] : 1.f;
+        z[0] = fmaf(z[0], g, x[0]);
+        write_row<F32, 1>(z, (char*)p.Y + o);
     }
 }
 
-// Tile shapes, features x tokens, as the projections take them (dfa_gemm.hip),
-// with the same rule between them: 64 x 64 and 128 x 128 rings while one tile
-// per CU covers the output, else 128 x 128 or 192 x 256 by the rounds they need.
+// Tile shapes, features x tokens, and the rule between them:
+//   64 x 64, ring      while one such tile per CU covers the output,
+//   128 x 128, ring    the same; beyond, by the rounds that each needs:
+//   128 x 128, stream  two workgroups per CU; a last round of one takes 0.65
+//   192 x 256, stream  1.38 of its round for 1.5 of its output
+//   256 x 256, stream  1.76 for 2, K a multiple of 128 (the others' registers
+//                      spill); not for a single round, whose output nothing
+//                      runs beside (12960 x 1152 -> 1152 with an fp32 residual:
+//                      73 us against 65 by 128 x 128)
+// us by 128, 192, 256: 32768 x 1152 -> 4608 396, 364, 342; 32768 x 4608 -> 1152
+// 360, 330, 353; 8192 x 1152 -> 4608 105, 103, 109.
 // Block order: the 32 or 64 workgroups that an XCD has resident share the lines
 // of their tiles in its L2; the fewest lines are in flight where they cover
 // about as many tokens as features.  Groups of 3 token tiles of 256 (measured
-// 1, 2, 3, 4, 8: 4096 x 1152 -> 4608 127, 126, 122, 130, 128 us; 32768 x 4608
+// 1, 2, 3, 4, 8: 8192 x 1152 -> 4608 127, 126, 122, 130, 128 us; 32768 x 4608
 // -> 1152 365, 366, 372, 369, 378; 32768 x 1152 -> 4608 381, 378, 367, 379,
 // 388) and of 4 of 128 (1, 4, 8: 8192 x 1152 -> 4608 139, 136, 146).
 using Tile64 = Tile<1, 1, 2, 2, 2, 4>;
 using Tile128Ring = Tile<2, 1, 2, 4, 1, 4>;
 using Tile128 = Tile<2, 2, 2, 2, 2>;
 using Tile192 = Tile<3, 2, 2, 4, 1>;
+using Tile256 = Tile<4, 2, 2, 4, 1>;
 
 template <int ACT, bool F32>
 hipError_t launch_tiles(LinearParams& p, hipStream_t stream) {
     p.group = 4;
     if (tiles<Tile64>(p) <= 256) return launch_shape<ACT, LinearOut<F32, Tile64>, Tile64>(p, stream);
-    const long long n128 = tiles<Tile128>(p), n192 = tiles<Tile192>(p);
+    const long long n128 = tiles<Tile128>(p);
     if (n128 <= 256) return launch_shape<ACT, LinearOut<F32, Tile128Ring>, Tile128Ring>(p, stream);
-    const long long last = n128 % 512;
-    const long long rounds128 = 100 * (n128 / 512) + (last == 0 ? 0 : (last <= 256 ? 65 : 100));
-    const long long rounds192 = 125 * ((n192 + 255) / 256);
-    if (rounds192 >= rounds128) return launch_shape<ACT, LinearOut<F32, Tile128>, Tile128>(p, stream);
+    const long long last = n128 % 512, rounds192 = (tiles<Tile192>(p) + 255) / 256, rounds256 = (tiles<Tile256>(p) + 255) / 256;
+    const long long cost128 = 100 * (n128 / 512) + (last == 0 ? 0 : (last <= 256 ? 65 : 100)), cost192 = 138 * rounds192;
+    const long long cost256 = rounds256 > 1 ? 176 * rounds256 : cost128;
+    if constexpr (ACT == ACT_ROWS) {
+        if (cost256 < cost128 && cost256 < cost192) {
+            p.group = 3;
+            return launch_shape<ACT, LinearOut<F32, Tile256>, Tile256>(p, stream);
+        }
+    }
+    if (cost128 <= cost192) return launch_shape<ACT, LinearOut<F32, Tile128>, Tile128>(p, stream);
     p.group = 3;
     return launch_shape<ACT, LinearOut<F32, Tile192>, Tile192>(p, stream);
 }
 
+template <bool F32, class T>
+hipError_t launch_any(LinearParams& p, hipStream_t stream) {
+    p.group = 4;
+    p.nft = (p.N + T::TF - 1) / T::TF;
+    const long long ntt = ((long long)p.M + T::TT - 1) / T::TT, nb = ntt * p.nft;
+    if (nb > (1LL << 23)) return hipErrorInvalidValue;
+    p.ntt = (int)ntt;
+    p.nblocks = (int)nb;
+    hipLaunchKernelGGL((linear_any_kernel<F32, T>), dim3(p.nblocks), dim3(T::NT), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <bool F32, int TB>
+hipError_t launch_few(LinearParams& p, hipStream_t stream) {
+    hipLaunchKernelGGL((linear_few_kernel<F32, TB>), dim3((p.N + 15) / 16), dim3(512), 0, stream, p);
+    return hipGetLastError();
+}
+
 template <bool F32>
 hipError_t launch(LinearParams& p, hipStream_t stream) {
-    if (p.H > 1 && p.K % (2 * GK) == 0) return launch_tiles<ACT_HEADS, F32>(p, stream);
-    if (p.H == 1 && p.K % (2 * GK) == 0) return launch_tiles<ACT_ROWS, F32>(p, stream);
-    if (p.H == 1 && p.K % 8 == 0) return launch_tiles<ACT_ROWS_TAIL, F32>(p, stream);
-    p.nft = (p.N + 63) / 64;
-    p.ntt = (p.M + 63) / 64;
-    const long long blocks = (long long)p.nft * p.ntt;
-    if (blocks > (1LL << 23)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(linear_general_kernel<F32>, dim3((unsigned)blocks), dim3(256), 0, stream, p);
-    return hipGetLastError();
+    fast_divisor(p.L, p.lmul, p.lshift);
+    fast_divisor(p.d, p.dmul, p.dshift);
+    // Few tokens: a workgroup per 16 features reads every token, so not beyond a
+    // workgroup per CU but for very few (us, against the next kernel: 2 tokens x
+    // 4608 -> 1152 8.3 and 15.3; 16 x 1152 -> 2304 5.1, 6.4; 32 x 1152 -> 2304 6.1,
+    // 6.7; 32 x 4608 -> 1152 15.0, 14.5; 2 x 1152 -> 6912 6.4, 6.6; 8 x 1152 -> 6912 7.0, 6.6).
+    const bool aligned = p.K % 8 == 0, narrow = !aligned || p.N <= 16 * 256;
+    if (p.M <= 4 || (narrow && p.M <= 16)) return launch_few<F32, 1>(p, stream);
+    if (narrow && p.M <= 32 && (!aligned || p.K <= 2304)) return launch_few<F32, 2>(p, stream);
+    const bool tail = p.K % (2 * GK) != 0;
+    if (p.H > 1) return tail ? launch_tiles<ACT_HEADS_TAIL, F32>(p, stream) : launch_tiles<ACT_HEADS, F32>(p, stream);
+    if (aligned) return tail ? launch_tiles<ACT_ROWS_TAIL, F32>(p, stream) : launch_tiles<ACT_ROWS, F32>(p, stream);
+    // 200 x 1001 -> 1153: 17 us; 8194 x 1001 -> 1153 by 128 x 128 tiles 58
+    if (tiles<Tile128>(p) <= 128) return launch_any<F32, Tile<1, 1, 2, 2, 2>>(p, stream);
+    return launch_any<F32, Tile128>(p, stream);
 }
 
 }  // namespace

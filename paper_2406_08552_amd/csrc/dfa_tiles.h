@@ -71,8 +71,11 @@ __device__ __forceinline__ int chunk_off(int row, int ch) { return row * GK + ((
 enum {
     ACT_ROWS = 0,        // activations: [M][K] rows, K a multiple of 128,
     ACT_ROWS_TAIL = 1,   // or of 8,
-    ACT_HEADS = 2        // or O [B][H][L][d], K = H d a multiple of 128
+    ACT_HEADS = 2,       // or O [B][H][L][d], K = H d a multiple of 128,
+    ACT_HEADS_TAIL = 3   // or of d
 };
+constexpr bool in_heads(int act) { return act == ACT_HEADS || act == ACT_HEADS_TAIL; }
+constexpr bool has_tail(int act) { return act == ACT_ROWS_TAIL || act == ACT_HEADS_TAIL; }
 
 // What a product W Act^T reads, and the order of its tiles.
 struct Operands {
@@ -87,7 +90,7 @@ struct Operands {
     int nblocks;
 };
 
-// What lanes copy whose chunk lies behind the end of a row (ACT_ROWS_TAIL).
+// What lanes copy whose chunk lies behind the end of a row (has_tail).
 __device__ __attribute__((aligned(16))) uint32_t zero_chunk[4];
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
@@ -113,9 +116,9 @@ struct Copier {
     uint32_t off[T::CPW];        // byte offset of the lane's chunk from its operand's uniform base
     const char* wbase;           // the uniform bases: W's first feature row of the tile, at the next k-tile,
     const char* abase;           // and (ACT_ROWS) the first token row
-    const char* ptr[ACT == ACT_HEADS ? T::CPW - T::CPF : 1];   // ACT_HEADS token rows: the lane's address
-    int j;                       // ACT_HEADS: dim of the lane's chunk within its head
-    int left;                    // ACT_ROWS_TAIL: elements of a row from the lane's chunk of the next k-tile on
+    const char* ptr[in_heads(ACT) ? T::CPW - T::CPF : 1];   // heads, token rows: the lane's address
+    int j;                       // heads: dim of the lane's chunk within its head
+    int left;                    // has_tail: elements of a row from the lane's chunk of the next k-tile on
     int wave, lrow, ch;
 
     __device__ __forceinline__ void init(int wave_, int lane) {
@@ -128,7 +131,7 @@ struct Copier {
     __device__ __forceinline__ void start(const Operands& p, int n0, int t0) {
         asm volatile("" : "+v"(lrow), "+v"(ch));
         wbase = (const char*)(p.W + (size_t)n0 * p.K);
-        abase = ACT != ACT_HEADS ? (const char*)(p.act + (size_t)t0 * p.K) : nullptr;
+        abase = !in_heads(ACT) ? (const char*)(p.act + (size_t)t0 * p.K) : nullptr;
         left = p.K - 8 * ch;
         j = 8 * ch;                                     // < d: d is at least 64
 #pragma unroll
@@ -139,7 +142,7 @@ struct Copier {
                 off[i] = (uint32_t)min(row, p.N - 1 - n0) * (uint32_t)(2 * p.K) + 16u * ch;
             } else {
                 const int tr = min((wave + i * T::NW) * 8 + lrow - T::TF, p.M - 1 - t0);
-                if constexpr (ACT != ACT_HEADS) {
+                if constexpr (!in_heads(ACT)) {
                     off[i] = (uint32_t)tr * (uint32_t)(2 * p.K) + 16u * ch;
                 } else {
                     const int t = t0 + tr, b = fast_div(t, p.lmul, p.lshift);
@@ -158,7 +161,7 @@ struct Copier {
         left = p.K - 8 * ch;
 #pragma unroll
         for (int i = 0; i < T::CPW; ++i) off[i] = 16u * ch;
-        if constexpr (ACT == ACT_HEADS) {
+        if constexpr (in_heads(ACT)) {
             j = 8 * ch;
 #pragma unroll
             for (int i = 0; i < T::CPW - T::CPF; ++i) ptr[i] = (const char*)p.act + 16 * ch;
@@ -176,8 +179,8 @@ struct Copier {
         for (int i = 0; i < T::CPW; ++i) {
             __attribute__((address_space(3))) void* to =
                 (__attribute__((address_space(3))) void*)(st + (wave + i * T::NW) * 8 * GK);
-            if constexpr (ACT == ACT_ROWS_TAIL) {
-                const char* from = (i < T::CPF ? wbase : abase) + off[i];
+            if constexpr (has_tail(ACT)) {
+                const char* from = i < T::CPF ? wbase + off[i] : in_heads(ACT) ? ptr[in_heads(ACT) ? i - T::CPF : 0] : abase + off[i];
                 __builtin_amdgcn_global_load_lds((const void*)(left > 0 ? from : (const char*)zero_chunk), to, 16, 0, 0);
             } else if (i < T::CPF)
                 __builtin_amdgcn_global_load_lds((const void*)(wbase + off[i]), to, 16, 0, 0);
@@ -186,17 +189,21 @@ struct Copier {
             else
                 __builtin_amdgcn_global_load_lds((const void*)ptr[i - T::CPF], to, 16, 0, 0);
         }
+        step(p, advance);
+    }
+    // to the next k-tile
+    __device__ __forceinline__ void step(const Operands& p, bool advance = true) {
         wbase += advance ? 2 * GK : 0;
-        if constexpr (ACT != ACT_HEADS) {
+        if constexpr (has_tail(ACT)) left -= advance ? GK : 0;
+        if constexpr (!in_heads(ACT)) {
             abase += advance ? 2 * GK : 0;
-            if constexpr (ACT == ACT_ROWS_TAIL) left -= advance ? GK : 0;
         } else {
             // the lane's chunk of the next k-tile, 64 features on, at most one head further (d >= 64)
             const bool w = j + GK >= p.d;
-            const long long step = advance ? 2 * GK + (w ? 2LL * ((long long)p.L * p.d - p.d) : 0) : 0;
+            const long long by = advance ? 2 * GK + (w ? 2LL * ((long long)p.L * p.d - p.d) : 0) : 0;
             j += advance ? GK - (w ? p.d : 0) : 0;
 #pragma unroll
-            for (int i = 0; i < T::CPW - T::CPF; ++i) ptr[i] += step;
+            for (int i = 0; i < T::CPW - T::CPF; ++i) ptr[i] += by;
         }
     }
 };
@@ -308,7 +315,7 @@ gemm_stream_kernel(typename OUT::Params p) {
 
     Copier<ACT, T> cp;
     cp.init(wave, lane);
-    const int nk = (p.K + 2 * GK - 1) / (2 * GK) * 2;  // even (ACT_ROWS_TAIL: the last ones hold zeros)
+    const int nk = (p.K + 2 * GK - 1) / (2 * GK) * 2;  // even (has_tail: the last ones hold zeros)
     // the biases of the wavefront's features, four to a lane
     f32x4 bv{0.f, 0.f, 0.f, 0.f};
     auto load_bias = [&](int n) {
@@ -448,7 +455,7 @@ gemm_ring_kernel(typename OUT::Params p) {
 
     Copier<ACT, T> cp;
     cp.init(wave, lane);
-    const int nk = (p.K + 2 * GK - 1) / (2 * GK) * 2;  // even (ACT_ROWS_TAIL: the last ones hold zeros)
+    const int nk = (p.K + 2 * GK - 1) / (2 * GK) * 2;  // even (has_tail: the last ones hold zeros)
     f32x4 bv[T::MB][4];
 #pragma unroll
     for (int mb = 0; mb < T::MB; ++mb)
