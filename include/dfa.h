@@ -245,7 +245,7 @@ dfa_status dfa_layer_norm(const void* X, const void* weight, const void* bias, v
  *   pass wrote them; weight as there
  *   dweight, dbias  fp32 [groups][C], each may be NULL.  groups = 1 sums over
  *                   the whole batch (the gradient of a row that it shares),
- *                   groups = B (at most 2^22) over each entry's tokens.
+ *                   groups = B (at most 2^21) over each entry's tokens.
  *   workspace       DEVICE buffer, 16-byte aligned, of at least
  *                   dfa_layer_norm_backward_workspace_bytes() bytes (NULL is
  *                   fine where that is 0 or both gradients are NULL); calls

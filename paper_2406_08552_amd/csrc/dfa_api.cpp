@@ -561,7 +561,7 @@ dfa_status dfa_layer_norm_backward(const void* dY, const void* X, const void* we
     if (groups != 1 && groups != B)
         return fail(DFA_ERR_INVALID_ARG, "groups=%d must be 1 or the batch (B=%d)", groups, B);
     if (groups > dfa::NORM_GROUPS_MAX)
-        return fail(DFA_ERR_INVALID_ARG, "groups=%d is too large (at most 2^22)", groups);
+        return fail(DFA_ERR_INVALID_ARG, "groups=%d is too large (at most 2^21)", groups);
     if ((st = check_ptr(dY, "dY")) != DFA_OK) return st;
     if ((st = check_ptr(X, "X")) != DFA_OK) return st;
     if ((st = check_ptr(dX, "dX")) != DFA_OK) return st;

@@ -68,7 +68,7 @@ struct NormGradLaunch {
     int B, L, C, groups;
 };
 constexpr int NORM_C_MAX = 16384;
-constexpr int NORM_GROUPS_MAX = 1 << 22;   // a workgroup each at least
+constexpr int NORM_GROUPS_MAX = 1 << 21;   // a workgroup of up to 1024 lanes each at least
 hipError_t launch_layer_norm(const NormLaunch& a, hipStream_t stream);
 hipError_t launch_layer_norm_backward(const NormGradLaunch& a, hipStream_t stream);
 // fp32 values of workspace that the weight's and the bias's gradients take.

@@ -182,48 +182,53 @@ __global__ void __launch_bounds__(T::NT) linear_any_kernel(LinearParams p) {
     __shared__ __attribute__((aligned(16))) uint16_t scratch[T::NW * Out::SCRATCH];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wf = wave % T::WF, wt = wave / T::WF, r32 = lane & 31, h = lane >> 5;
-    int n0, t0;
-    const int x = blockIdx.x & 7, q = p.nblocks >> 3, rem = p.nblocks & 7;
-    tile_origin<T>(p, x * q + min(x, rem) + ((int)blockIdx.x >> 3), n0, t0);
     const int row = tid >> 3, ch = tid & 7;           // and the rows NT / 8 apart
-    u32x4 v[CH];
-    auto load = [&](int k0) {
-        const int k = k0 + 8 * ch;
+    const int ao = chunk_off(32 * T::MB * wf + r32, h), bo = chunk_off(T::TF + 32 * T::NB * wt + r32, h);
+    const int nk = (p.K + GK - 1) / GK;
+    // a contiguous range of tiles per XCD, as in gemm_stream_kernel
+    const int x = blockIdx.x & 7, q = p.nblocks >> 3, rem = p.nblocks & 7;
+    const int end = (x + 1) * q + min(x + 1, rem), stride = ((int)gridDim.x + 7 - x) >> 3;
+    for (int blk = x * q + min(x, rem) + ((int)blockIdx.x >> 3); blk < end; blk += stride) {
+        int n0, t0;
+        tile_origin<T>(p, blk, n0, t0);
+        u32x4 v[CH];
+        auto load = [&](int k0) {
+            const int k = k0 + 8 * ch;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int r = row + i * (T::NT / 8);
-            v[i] = u32x4{0, 0, 0, 0};
-            if (k < p.K) {
-                const uint16_t* from = r < T::TF ? p.W + (size_t)min(n0 + r, p.N - 1) * p.K + k
-                                                 : p.act + (size_t)min(t0 + r - T::TF, p.M - 1) * p.K + k;
-                v[i] = load8(from, p.K - k);
+            for (int i = 0; i < CH; ++i) {
+                const int r = row + i * (T::NT / 8);
+                v[i] = u32x4{0, 0, 0, 0};
+                if (k < p.K) {
+                    const uint16_t* from = r < T::TF ? p.W + (size_t)min(n0 + r, p.N - 1) * p.K
+                                                     : p.act + (size_t)min(t0 + r - T::TF, p.M - 1) * p.K;
+                    v[i] = load8(from + k, p.K - k);
+                }
+            }
+        };
+        f32x16 acc[T::MB][T::NB];
+        zero_acc<T>(acc);
+        load(0);
+        for (int kt = 0; kt < nk; ++kt) {
+            uint16_t* cur = st[kt & 1];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) *(u32x4*)(cur + chunk_off(row + i * (T::NT / 8), ch)) = v[i];
+            __syncthreads();   // behind it every wavefront has read the k-tile before this one
+            if (kt + 1 < nk) load((kt + 1) * GK);
+            Frag<T> f;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                f.read(cur, ks, ao, bo);
+                mma<T, 0, T::MB * T::NB>(acc, f);
             }
         }
-    };
-    f32x16 acc[T::MB][T::NB];
-    zero_acc<T>(acc);
-    const int ao = chunk_off(32 * T::MB * wf + r32, h), bo = chunk_off(T::TF + 32 * T::NB * wt + r32, h);
-    load(0);
-    const int nk = (p.K + GK - 1) / GK;
-    for (int kt = 0; kt < nk; ++kt) {
-        uint16_t* cur = st[kt & 1];
-#pragma unroll
-        for (int i = 0; i < CH; ++i) *(u32x4*)(cur + chunk_off(row + i * (T::NT / 8), ch)) = v[i];
-        __syncthreads();   // behind it every wavefront has read the k-tile before this one
-        if (kt + 1 < nk) load((kt + 1) * GK);
-        Frag<T> f;
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            f.read(cur, ks, ao, bo);
-            mma<T, 0, T::MB * T::NB>(acc, f);
-        }
+        const bool whole = n0 + T::TF <= p.N && t0 + T::TT <= p.M;
+        const int nw0 = n0 + 32 * T::MB * wf, tw0 = t0 + 32 * T::NB * wt;
+        Out out;
+        out.ahead(p, nw0, tw0, lane, whole);
+        if (whole) out.template store<true>(p, acc, scratch + wave * Out::SCRATCH, nw0, tw0, lane);
+        else out.template store<false>(p, acc, scratch + wave * Out::SCRATCH, nw0, tw0, lane);
+        __syncthreads();       // the last k-tile has been read, too
     }
-    const bool whole = n0 + T::TF <= p.N && t0 + T::TT <= p.M;
-    const int nw0 = n0 + 32 * T::MB * wf, tw0 = t0 + 32 * T::NB * wt;
-    Out out;
-    out.ahead(p, nw0, tw0, lane, whole);
-    if (whole) out.template store<true>(p, acc, scratch + wave * Out::SCRATCH, nw0, tw0, lane);
-    else out.template store<false>(p, acc, scratch + wave * Out::SCRATCH, nw0, tw0, lane);
 }
 
 // Few tokens (at most 16 TB): the weights' stream from HBM counts.  A workgroup
@@ -338,10 +343,11 @@ hipError_t launch_any(LinearParams& p, hipStream_t stream) {
     p.group = 4;
     p.nft = (p.N + T::TF - 1) / T::TF;
     const long long ntt = ((long long)p.M + T::TT - 1) / T::TT, nb = ntt * p.nft;
-    if (nb > (1LL << 23)) return hipErrorInvalidValue;
+    if (nb > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     p.ntt = (int)ntt;
     p.nblocks = (int)nb;
-    hipLaunchKernelGGL((linear_any_kernel<F32, T>), dim3(p.nblocks), dim3(T::NT), 0, stream, p);
+    const int grid = (int)(nb < 256 * T::WGS ? nb : 256 * T::WGS);
+    hipLaunchKernelGGL((linear_any_kernel<F32, T>), dim3(grid), dim3(T::NT), 0, stream, p);
     return hipGetLastError();
 }
 

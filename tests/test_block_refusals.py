@@ -66,7 +66,7 @@ def grad(L, dY=RES, X=X, w=W, mean=M1, rstd=M2, dX=Y, dw=BIAS, db=GATE, ws=WS, n
     (dict(nws=16), INVALID, "too small"),
     (dict(groups=0), INVALID, "groups"),
     (dict(groups=3), INVALID, "groups"),
-    (dict(B=1 << 23, l=1, groups=1 << 23), INVALID, "2^22"),
+    (dict(B=1 << 23, l=1, groups=1 << 23), INVALID, "2^21"),
     (dict(xt=-1), INVALID, "x_type"),
     (dict(C=20000), UNSUPPORTED, "16384"),
     (dict(dX=X), INVALID, "overlaps"),
