@@ -119,8 +119,10 @@ struct LinearOut {
                                 if (WHOLE || f + e < p.N) g[e] = gp[e];
                         }
                     }
+                    if (p.gate.p || p.residual) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) z[e] = fmaf(z[e], g[e], x[e]);
+                        for (int e = 0; e < E; ++e) z[e] = fmaf(z[e], g[e], x[e]);
+                    }
                     if (full) {
                         write_row<F32, E>(z, out + at);
                     } else {
