@@ -263,7 +263,7 @@ size_t dfa_layer_norm_backward_workspace_bytes(int B, int L, int C, int groups);
 /* Activations of a linear layer. */
 enum {
     DFA_ACT_NONE = 0,
-    DFA_ACT_GELU = 1,        /* z * Phi(z), Phi the normal distribution function */
+    DFA_ACT_GELU = 1,        /* z * Phi(z), Phi the normal distribution function (to 3e-7) */
     DFA_ACT_GELU_TANH = 2,   /* z / 2 * (1 + tanh(sqrt(2 / pi) * (z + 0.044715 z^3))) */
     DFA_ACT_SILU = 3         /* z / (1 + exp(-z)) */
 };

@@ -2,7 +2,12 @@
 // fp32 from the accumulators to the one rounding of Y.
 //
 // The main loops are those of dfa_tiles.h; here are their output, the
-// kernels for other cases, and the rule between them.
+// kernels for other cases, and the rule between them.  Few tokens are a stream
+// of the weights (2 x 1152 -> 6912 5.8 us, of which a launch takes 3.3).  Many are bound by
+// the copies of the k-tiles into LDS and the clock that power leaves: 8192 x
+// 1152 -> 4608 with GELU 110 us (789 TFLOP/s), 32768 x 4608 -> 1152 with gate and
+// fp32 residual 370 us (940 TFLOP/s); the second in fp32 read and written is
+// also 302 MB, which leave beside the next tile's products.
 #include "dfa_epilogue.h"
 #include "dfa_tiles.h"
 
@@ -174,8 +179,8 @@ struct TokenRow {
     }
 };
 
-// Any K: rows that 16 bytes do not divide take no direct copies, so the k-tiles pass through registers, the next one in
-// flight while this one is multiplied.
+// Any K: rows that 16 bytes do not divide take no direct copies, so the k-tiles
+// pass through registers, the next one in flight while this one is multiplied.
 template <bool F32, class T>
 __global__ void __launch_bounds__(T::NT) linear_any_kernel(LinearParams p) {
     constexpr int CH = (T::TF + T::TT) * 8 / T::NT;   // chunks of eight k per lane and k-tile
@@ -298,8 +303,13 @@ __global__ void __launch_bounds__(512) linear_few_kernel(LinearParams p) {
 }
 
 // Tile shapes, features x tokens, and the rule between them:
-//   64 x 64, ring      while one such tile per CU covers the output,
-//   128 x 128, ring    the same; beyond, by the rounds that each needs:
+//   64 x 64, ring      while two such tiles per CU cover the output, which a CU
+//                      holds at once (us against the next: 602 x 1152 -> 1152 7.0
+//                      and 12.4, 1790 x 1152 -> 1152 11.6 and 13.2, 1024 x 4608 ->
+//                      1152 39 and 46; with more tiles 2000 x 1152 -> 1152 15.4, 13.3)
+//   128 x 128, ring    while one per CU does (2000 x 1152 -> 1152 13.3, stream 16.7;
+//                      3600 x 1152 -> 1152 25.1, stream 19.2); beyond, by the
+//                      rounds that each needs:
 //   128 x 128, stream  two workgroups per CU; a last round of one takes 0.65
 //   192 x 256, stream  1.38 of its round for 1.5 of its output
 //   256 x 256, stream  1.76 for 2, K a multiple of 128 (the others' registers
@@ -323,7 +333,7 @@ using Tile256 = Tile<4, 2, 2, 4, 1>;
 template <int ACT, bool F32>
 hipError_t launch_tiles(LinearParams& p, hipStream_t stream) {
     p.group = 4;
-    if (tiles<Tile64>(p) <= 256) return launch_shape<ACT, LinearOut<F32, Tile64>, Tile64>(p, stream);
+    if (tiles<Tile64>(p) <= 512) return launch_shape<ACT, LinearOut<F32, Tile64>, Tile64>(p, stream);
     const long long n128 = tiles<Tile128>(p);
     if (n128 <= 256) return launch_shape<ACT, LinearOut<F32, Tile128Ring>, Tile128Ring>(p, stream);
     const long long last = n128 % 512, rounds192 = (tiles<Tile192>(p) + 255) / 256, rounds256 = (tiles<Tile256>(p) + 255) / 256;
@@ -373,7 +383,8 @@ hipError_t launch(LinearParams& p, hipStream_t stream) {
     const bool tail = p.K % (2 * GK) != 0;
     if (p.H > 1) return tail ? launch_tiles<ACT_HEADS_TAIL, F32>(p, stream) : launch_tiles<ACT_HEADS, F32>(p, stream);
     if (aligned) return tail ? launch_tiles<ACT_ROWS_TAIL, F32>(p, stream) : launch_tiles<ACT_ROWS, F32>(p, stream);
-    // 200 x 1001 -> 1153: 17 us; 8194 x 1001 -> 1153 by 128 x 128 tiles 58
+    // 64 x 64 tiles against 128 x 128, 1001 -> 1153, us: 200 tokens 16.6 and 26.0, 1000 17.0 and 25.3, 2000 30.7 and
+    // 26.0, 8194 87 and 57
     if (tiles<Tile128>(p) <= 128) return launch_any<F32, Tile<1, 1, 2, 2, 2>>(p, stream);
     return launch_any<F32, Tile128>(p, stream);
 }

@@ -8,8 +8,14 @@
 // sum of squared differences (two passes, so that a large mean costs nothing)
 // and the result are formed in fp32, and leaves once.  Up to 1280 features a
 // wavefront holds a row, 20 values a lane at most; beyond, a workgroup of
-// four or sixteen wavefronts.  A wavefront walks several rows of a batch entry, whose
-// weights it keeps, and reads the next row while it works on this one.
+// four or sixteen wavefronts (1152 features by four: 32768 tokens 54 us against
+// 49, gradients of 8192 32 against 19; 4096 features by sixteen: 60 against 44).
+// A wavefront walks several rows of a batch entry, whose weights it keeps, and
+// reads the next row while it works on this one.
+//
+// 32768 tokens x 1152 fp32 to bf16 take 49 us, 4.6 TB/s where a large copy
+// reaches 5.1; the gradients of 8192 tokens x 1152 bf16 15 us, 3.7 TB/s, of
+// which 4 us are the second kernel's, which adds up the workgroups' sums.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -122,7 +128,8 @@ __device__ __forceinline__ void store_row(const float (&x)[S::NV][S::V], void* r
         } else {
             uint32_t u[S::V / 2];
 #pragma unroll
-            for (int i = 0; i < S::V / 2; ++i) u[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[k][2 * i], (__bf16)x[k][2 * i + 1]});
+            for (int i = 0; i < S::V / 2; ++i)
+                u[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[k][2 * i], (__bf16)x[k][2 * i + 1]});
             __builtin_memcpy(to, u, 2 * S::V);
         }
     }

@@ -19,8 +19,8 @@
 //     k-tiles runs on from one tile to the next: the next tile's first copies
 //     are in flight while this one's output leaves, and its stores drain under
 //     the next tile's MFMAs.
-//   gemm_ring_kernel  grids of at most a workgroup per CU, where only depth
-//     hides the copies' latency: four stages, one tile per workgroup.
+//   gemm_ring_kernel  grids that fit at once, where only depth hides the copies'
+//     latency: four stages, one tile per workgroup.
 #ifndef DFA_TILES_H
 #define DFA_TILES_H
 
@@ -180,7 +180,9 @@ struct Copier {
             __attribute__((address_space(3))) void* to =
                 (__attribute__((address_space(3))) void*)(st + (wave + i * T::NW) * 8 * GK);
             if constexpr (has_tail(ACT)) {
-                const char* from = i < T::CPF ? wbase + off[i] : in_heads(ACT) ? ptr[in_heads(ACT) ? i - T::CPF : 0] : abase + off[i];
+                const char* from = i < T::CPF     ? wbase + off[i]
+                                   : in_heads(ACT) ? ptr[in_heads(ACT) ? i - T::CPF : 0]
+                                                   : abase + off[i];
                 __builtin_amdgcn_global_load_lds((const void*)(left > 0 ? from : (const char*)zero_chunk), to, 16, 0, 0);
             } else if (i < T::CPF)
                 __builtin_amdgcn_global_load_lds((const void*)(wbase + off[i]), to, 16, 0, 0);

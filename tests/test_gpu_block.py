@@ -257,7 +257,7 @@ def _route(B, L, K, N, heads=1):
         return "few 32"
     if K % 8:
         return "any 64" if t(128, 128) <= 128 else "any 128"
-    if t(64, 64) <= 256:
+    if t(64, 64) <= 512:
         return "64 ring"
     n = t(128, 128)
     if n <= 256:
@@ -275,7 +275,8 @@ def _route(B, L, K, N, heads=1):
     (2, 1100, 128, 1030, 1, "128 ring"), (2, 1100, 1000, 1030, 1, "128 ring"), (3, 100, 999, 333, 1, "any 64"), (1, 3000, 129, 901, 1, "any 128"),
     (2, 6000, 128, 1100, 1, "128"), (12, 1000, 328, 1099, 1, "128"), (1, 8200, 128, 1160, 1, "192"), (1, 8200, 136, 1153, 1, "192"),
     (1, 16100, 384, 2041, 1, "256"), (1, 16128, 128, 2048, 1, "256"), (2, 1100, 128, 1030, 2, "128 ring"), (12, 1000, 320, 1100, 5, "128"),
-    (3, 2700, 192, 1160, 3, "192"), (1, 8200, 1152, 1153, 16, "192"), (2, 150, 216, 515, 3, "64 ring")])
+    (3, 2700, 192, 1160, 3, "192"), (1, 8200, 1152, 1153, 16, "192"), (2, 150, 216, 515, 3, "64 ring"),
+    (1, 1790, 136, 1150, 1, "64 ring"), (3, 596, 216, 1150, 3, "64 ring"), (1, 1793, 136, 1153, 1, "128 ring")])
 def test_linear_routes(B, L, K, N, heads, route):
     assert _route(B, L, K, N, heads) == route, "not the route this case is for"
     for ytype in (BF16, F32):
