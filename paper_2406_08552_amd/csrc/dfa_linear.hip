@@ -3,11 +3,11 @@
 //
 // The main loops are those of dfa_tiles.h; here are their output, the
 // kernels for other cases, and the rule between them.  Few tokens are a stream
-// of the weights (2 x 1152 -> 6912 5.8 us, of which a launch takes 3.3).  Many are bound by
-// the copies of the k-tiles into LDS and the clock that power leaves: 8192 x
-// 1152 -> 4608 with GELU 110 us (789 TFLOP/s), 32768 x 4608 -> 1152 with gate and
-// fp32 residual 370 us (940 TFLOP/s); the second in fp32 read and written is
-// also 302 MB, which leave beside the next tile's products.
+// of the weights (2 x 1152 -> 6912 5.8 us, of which a launch takes 3.3).  Many
+// are bound by the copies of the k-tiles into LDS and the clock that power
+// leaves: 8192 x 1152 -> 4608 with GELU's tanh form 110 us (789 TFLOP/s), 32768 x
+// 4608 -> 1152 with gate and fp32 residual 370 us (940 TFLOP/s), 302 MB of
+// residual and output among it, which move beside the next tile's products.
 #include "dfa_epilogue.h"
 #include "dfa_tiles.h"
 

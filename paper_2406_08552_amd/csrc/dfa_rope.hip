@@ -11,8 +11,7 @@
 // fractions of -1/2 to 1/2.
 //
 // 16 heads of d = 72 at 2 x 16384 tokens, halves, take 59 us for Q and K, 302 MB
-// at 5.1 TB/s, the rate of a large copy; 24 heads of d = 64 at 16384 tokens, pairs,
-// 25 us (4.8 TB/s).
+// at 5.1 TB/s, the rate of a large copy; at 2 x 6480 tokens, pairs, 25 us (4.8 TB/s).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -26,8 +25,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-// heads whose loads a lane has in flight (2, 4, 8: 2048 tokens x 16 heads 8.8, 8.3,
-// 9.4 us; 32768 x 16 heads 60, 60, 66)
+// heads whose loads a lane has in flight (2, 4, 8, d = 72, 16 heads of Q and of K: 2048
+// tokens 8.8, 8.3, 9.4 us; 32768 60, 60, 66)
 constexpr int BATCH = 4;
 constexpr uint8_t KEEP = 255;   // "axis" of the dims behind the last section
 
@@ -262,8 +261,8 @@ __global__ void __launch_bounds__(THREADS) rope_units_kernel(RopeParams p) {
 dim3 grid_of(RopeParams& p) {
     const int nh = p.heads[0] + p.heads[1];
     const long long tiles = ((long long)p.L + p.tokens - 1) / p.tokens;
-    // 2048 workgroups at least: fewer heads each, down to one batch of loads (1024, 2048, 4096: 16384 tokens x 48 heads
-    // 27.9, 25.9, 28.1 us; 32768 x 32 heads 65, 61, 60)
+    // 2048 workgroups at least: fewer heads each, down to one batch of loads (1024, 2048, 4096, 16 heads of Q and of K:
+    // 12960 tokens 27.9, 25.9, 28.1 us; 32768 65, 61, 60)
     long long parts = (2047 + tiles * p.B) / (tiles * p.B);
     if (parts > (nh + BATCH - 1) / BATCH) parts = (nh + BATCH - 1) / BATCH;
     if (parts > 65535) parts = 65535;
