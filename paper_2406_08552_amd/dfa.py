@@ -17,6 +17,7 @@ themselves (the ABI tests do).
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import numpy as np
@@ -346,10 +347,18 @@ def _rows(t, B, C, name) -> int:
     return t.stride(0) if t.dim() == 2 and B > 1 else 0
 
 
+def _int32(n, name) -> int:
+    """An integer of any type; ctypes would take the low 32 bits of a larger one."""
+    n = operator.index(n)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{name}={n} is too large")
+    return n
+
+
 def _tokens(t, name):
     if t.dim() != 3:
         raise ValueError(f"{name}: expected a [B, L, C] tensor, got {tuple(t.shape)}")
-    return tuple(t.shape)
+    return tuple(_int32(n, f"a size of {name}") for n in t.shape)
 
 
 def dfa_layer_norm(X, weight, bias, Y, mean=None, rstd=None, eps: float = 1e-6, weight_offset: float = 0.0,
@@ -375,7 +384,7 @@ def dfa_layer_norm(X, weight, bias, Y, mean=None, rstd=None, eps: float = 1e-6, 
 
 def layer_norm_backward_workspace_bytes(B: int, L: int, C: int, groups: int = 1) -> int:
     """groups: rows of dweight and dbias, 1 or B."""
-    return int(lib().dfa_layer_norm_backward_workspace_bytes(B, L, C, groups))
+    return int(lib().dfa_layer_norm_backward_workspace_bytes(*[_int32(n, "a size") for n in (B, L, C, groups)]))
 
 
 def dfa_layer_norm_backward(dY, X, weight, mean, rstd, dX, dweight, dbias, workspace=None, weight_offset: float = 0.0,
@@ -419,13 +428,15 @@ def dfa_linear(X, W, bias, Y, act: int = ACT_NONE, gate=None, residual=None, str
     torch = _torch()
     if X.dim() == 4:
         B, H, L, d = X.shape
+        for n in (B, H, L, H * d):
+            _int32(n, "a size of X")
         K = H * d
     else:
         B, L, K = _tokens(X, "X")
         H = 1
     if Y.dim() != 3 or tuple(Y.shape[:2]) != (B, L):
         raise ValueError(f"Y {tuple(Y.shape)} does not match [B, L, N] with B={B}, L={L}")
-    N = Y.shape[2]
+    N, act = _int32(Y.shape[2], "N"), _int32(act, "act")
     yt = _stream_type(Y, "Y")
     _same_device((X, "X"), (W, "W"), (bias, "bias"), (Y, "Y"), (gate, "gate"), (residual, "residual"))
     _expect(X, torch.bfloat16, X.shape, "X")
@@ -434,7 +445,7 @@ def dfa_linear(X, W, bias, Y, act: int = ACT_NONE, gate=None, residual=None, str
     _expect(Y, Y.dtype, (B, L, N), "Y")
     _expect(residual, Y.dtype, (B, L, N), "residual")
     gs = _rows(gate, B, N, "gate")
-    _check(lib().dfa_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), _ptr(Y), int(act), yt, B, L, H, K, N, gs,
+    _check(lib().dfa_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(gate), _ptr(residual), _ptr(Y), act, yt, B, L, H, K, N, gs,
                             _stream(stream)))
 
 
@@ -450,21 +461,22 @@ def dfa_rope(Q, K, Qout, Kout, pos, sections, base: float = 10000.0, interleaved
     torch = _torch()
     if Q.dim() != 4:
         raise ValueError(f"Q: expected a [B, H, L, d] tensor, got {tuple(Q.shape)}")
-    B, Hq, L, d = Q.shape
+    B, Hq, L, d = (_int32(n, "a size of Q") for n in Q.shape)
     if (K is None) != (Kout is None):
         raise ValueError("give K and Kout, or neither")
     Hk = 0
     if K is not None:
         if K.dim() != 4 or (K.shape[0], K.shape[2], K.shape[3]) != (B, L, d):
             raise ValueError(f"K {tuple(K.shape)} does not match Q {tuple(Q.shape)}")
-        Hk = K.shape[1]
+        Hk = _int32(K.shape[1], "heads of K")
+    A = len(sections)
+    sec = (ctypes.c_int32 * max(A, 1))(*[_int32(n, "a section") for n in sections])
     _same_device((Q, "Q"), (K, "K"), (Qout, "Qout"), (Kout, "Kout"), (pos, "pos"))
     for t, heads, name in ((Q, Hq, "Q"), (Qout, Hq, "Qout"), (K, Hk, "K"), (Kout, Hk, "Kout")):
         _expect(t, torch.bfloat16, (B, heads, L, d), name)
-    A = len(sections)
-    _expect(pos, torch.float32, (B, L, A) if pos.dim() == 3 else (L, A), "pos")
-    stride = L * A if pos.dim() == 3 and B > 1 else 0
-    sec = (ctypes.c_int32 * max(A, 1))(*[int(n) for n in sections])
+    each = pos is not None and pos.dim() == 3
+    _expect(pos, torch.float32, (B, L, A) if each else (L, A), "pos")
+    stride = L * A if each and B > 1 else 0
     _check(lib().dfa_rope(_ptr(Q), _ptr(K), _ptr(Qout), _ptr(Kout), _ptr(pos), sec, A, float(base), int(bool(interleaved)),
                           int(bool(inverse)), B, Hq, Hk, L, d, stride, _stream(stream)))
 

@@ -181,3 +181,30 @@ def test_binding_refuses_host_tensors():
         dfa.dfa_layer_norm(t[0], v, v, t)
     with pytest.raises(ValueError, match="neither"):
         dfa.dfa_rope(h, h, h, None, torch.zeros(4, 2), [8, 8])
+
+
+def test_binding_refuses_sizes_past_32_bits():
+    """The C ABI's sizes are int: a larger one must not arrive as its low bits."""
+    big = (1 << 32) + 8
+    m = lambda *n, dtype=torch.bfloat16: torch.empty(n, dtype=dtype, device="meta")  # noqa: E731
+    v = torch.zeros(64)
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_layer_norm(m(1, big, 64), v, v, m(1, big, 64))
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_layer_norm_backward(m(1, big, 64), m(1, big, 64), v, v, v, m(1, big, 64), v, v)
+    with pytest.raises(ValueError, match="too large"):
+        dfa.layer_norm_backward_workspace_bytes(1, big, 64)
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_linear(m(1, 4, big), m(64, big), v, m(1, 4, 64))
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_linear(m(1, 1 << 28, 4, 64), m(64, 1 << 34), v, m(1, 4, 64))
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_linear(m(1, 4, 64), m(big, 64), None, m(1, 4, big))
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_linear(m(1, 4, 64), m(64, 64), v, m(1, 4, 64), act=1 << 32)
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_rope(m(1, 2, big, 8), None, m(1, 2, big, 8), None, m(big, 1, dtype=torch.float32), [8])
+    with pytest.raises(ValueError, match="too large"):
+        dfa.dfa_rope(m(1, 2, 4, 8), None, m(1, 2, 4, 8), None, m(4, 1, dtype=torch.float32), [big])
+    with pytest.raises(TypeError):
+        dfa.dfa_rope(m(1, 2, 4, 8), None, m(1, 2, 4, 8), None, m(4, 1, dtype=torch.float32), [7.5])
