@@ -318,7 +318,9 @@ __global__ void __launch_bounds__(S::NT) norm_grad_kernel(NormParams p) {
 }
 
 // dweight and dbias of a group: the sums of its splits' partial sums.  16
-// wavefronts read every 16th split of 64 columns, then are added in order.
+// wavefronts read every 16th split of 64 columns, AT of them in flight, then
+// are added in order.
+template <int AT>
 __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, float* dweight, float* dbias, int C, int splits) {
     __shared__ float s[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -326,8 +328,13 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, fl
     const float* from = partial + (size_t)blockIdx.y * splits * 2 * C + col;
     float v = 0.f;
     if (col < 2 * C) {
-#pragma unroll 4
-        for (int i = wave; i < splits; i += 16) v += from[(size_t)i * 2 * C];
+        for (int i = wave; i < splits; i += 16 * AT) {
+            float x[AT];   // behind the end the last one again, which is not added
+#pragma unroll
+            for (int j = 0; j < AT; ++j) x[j] = from[(size_t)min(i + 16 * j, splits - 1) * 2 * C];
+#pragma unroll
+            for (int j = 0; j < AT; ++j) v += i + 16 * j < splits ? x[j] : 0.f;
+        }
     }
     s[wave][lane] = v;
     __syncthreads();
@@ -346,14 +353,17 @@ constexpr int FORWARD_ROWS = 4;  // forward
 // group's tokens in the backward pass.  A workgroup per CU and 2 rows per
 // wavefront at least: more workgroups leave more partial sums (8192 tokens x
 // 1152, bf16: 256 workgroups of eight wavefronts 19.0 us, 512 of eight 23.0, 512
-// of four 19.2, 768 of four 20.0).
+// of four 19.2, 768 of four 20.0).  Two per CU up to 256 features, whose rows
+// are so short that latency counts (30798 x 191: 1 per CU 22, 2 18.0, 4 17.8 us;
+// 20000 x 64 12.6, 11.3, 14.2; 16000 x 512 17.7, 21 with 2).
 struct Split {
     int rows, splits;
 };
 Split grad_split(int B, int L, int C, int groups) {
     const long long group_rows = (long long)B * L / groups;
     const int block = C <= WIDE ? GRAD_ROWS : 1;
-    long long splits = (256 + groups - 1) / groups;
+    const int slots = C <= 256 ? 512 : 256;
+    long long splits = (slots + groups - 1) / groups;
     long long rows = (group_rows + splits * block - 1) / (splits * block);
     if (rows < 2) rows = 2;
     splits = (group_rows + rows * block - 1) / (rows * block);
@@ -380,6 +390,7 @@ hipError_t run_grad(NormParams& p, int groups, hipStream_t stream) {
 // of the two tensors, single elements below one vector.
 template <int ROWS, bool EXACT, class F>
 hipError_t by_width(int C, F&& run) {
+    if (C <= 256) return run(Shape<4, 1, 1, ROWS, EXACT>{});
     if (C <= 512) return run(Shape<4, 2, 1, ROWS, EXACT>{});
     if (C <= WIDE) return run(Shape<4, 5, 1, ROWS, EXACT>{});
     if (C <= 2048) return run(Shape<4, 2, 4, ROWS, EXACT>{});
@@ -445,8 +456,10 @@ hipError_t launch_layer_norm_backward(const NormGradLaunch& a, hipStream_t strea
         return a.x_f32 ? run_grad<true, decltype(s)>(p, a.groups, stream) : run_grad<false, decltype(s)>(p, a.groups, stream);
     });
     if (e != hipSuccess || !two) return e;
-    hipLaunchKernelGGL(norm_sum_kernel, dim3((2 * a.C + 63) / 64, a.groups), dim3(1024), 0, stream, a.partial, a.dweight,
-                       a.dbias, a.C, split.splits);
+    // 256 splits: 16 in flight take 0.6 to 1.1 us less than 4; 32 splits: 1.5 us more
+    const auto sum = split.splits <= 64 ? norm_sum_kernel<4> : norm_sum_kernel<16>;
+    hipLaunchKernelGGL(sum, dim3((2 * a.C + 63) / 64, a.groups), dim3(1024), 0, stream, a.partial, a.dweight, a.dbias, a.C,
+                       split.splits);
     return hipGetLastError();
 }
 
