@@ -238,8 +238,8 @@ __global__ void __launch_bounds__(T::NT) linear_any_kernel(LinearParams p) {
     }
 }
 
-// Few tokens (at most 16 TB): the weights' stream from HBM counts.  A workgroup
-// takes 16 features; its wavefronts take the 64-element pieces of K in turn,
+// Few tokens: the weights' stream from HBM counts.  Few outputs: the length of K.
+// A workgroup takes 16 features of 16 TB tokens; its wavefronts take the 64-element pieces of K in turn,
 // straight into registers (16 features x 128 bytes, AHEAD pieces in flight),
 // through v_mfma_f32_16x16x32_bf16 (A element e = A[l % 16][8 (l / 16) + e], B
 // alike, output element i = D[4 (l / 16) + i][l % 16]), and add up in LDS.
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(512) linear_few_kernel(LinearParams p) {
     constexpr int NW = 8, AHEAD = TB > 1 ? 2 : 3;
     __shared__ float sums[NW][TB][16][17];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r = lane & 15, kq = 8 * (lane >> 4), n0 = 16 * blockIdx.x;
+    const int r = lane & 15, kq = 8 * (lane >> 4), n0 = 16 * blockIdx.x, t0 = 16 * TB * blockIdx.y;
     const uint16_t* w = p.W + (size_t)min(n0 + r, p.N - 1) * p.K;
     f32x4 acc[TB];
 #pragma unroll
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(512) linear_few_kernel(LinearParams p) {
 #pragma unroll
             for (int tb = 0; tb < TB; ++tb) {
                 xv[slot][i][tb] = u32x4{0, 0, 0, 0};
-                if (k < p.K) xv[slot][i][tb] = load8(TokenRow(p, min(16 * tb + r, p.M - 1)).at(p, k), p.K - k);
+                if (k < p.K) xv[slot][i][tb] = load8(TokenRow(p, min(t0 + 16 * tb + r, p.M - 1)).at(p, k), p.K - k);
             }
         }
     };
@@ -287,11 +287,11 @@ __global__ void __launch_bounds__(512) linear_few_kernel(LinearParams p) {
         for (int i = 0; i < 4; ++i) sums[wave][tb][4 * (lane >> 4) + i][r] = acc[tb][i];
     __syncthreads();
     for (int e = threadIdx.x; e < TB * 256; e += 512) {
-        const int t = e >> 4, f = n0 + (e & 15);
+        const int lt = e >> 4, t = t0 + lt, f = n0 + (e & 15);
         if (t >= p.M || f >= p.N) continue;
         float z[1] = {0.f}, x[1] = {0.f};
 #pragma unroll
-        for (int i = 0; i < NW; ++i) z[0] += sums[i][t >> 4][t & 15][e & 15];
+        for (int i = 0; i < NW; ++i) z[0] += sums[i][lt >> 4][lt & 15][e & 15];
         if (p.bias) z[0] += p.bias[f];
         const size_t o = ((size_t)t * p.N + f) * (F32 ? 4 : 2);
         if (p.residual) read_row<F32, 1>(x, (const char*)p.residual + o);
@@ -365,7 +365,7 @@ hipError_t launch_any(LinearParams& p, hipStream_t stream) {
 
 template <bool F32, int TB>
 hipError_t launch_few(LinearParams& p, hipStream_t stream) {
-    hipLaunchKernelGGL((linear_few_kernel<F32, TB>), dim3((p.N + 15) / 16), dim3(512), 0, stream, p);
+    hipLaunchKernelGGL((linear_few_kernel<F32, TB>), dim3((p.N + 15) / 16, (p.M + 16 * TB - 1) / (16 * TB)), dim3(512), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -379,7 +379,15 @@ hipError_t launch(LinearParams& p, hipStream_t stream) {
     // 6.7; 32 x 4608 -> 1152 15.0, 14.5; 2 x 1152 -> 6912 6.4, 6.6; 8 x 1152 -> 6912 7.0, 6.6).
     const bool aligned = p.K % 8 == 0, narrow = !aligned || p.N <= 16 * 256;
     if (p.M <= 4 || (narrow && p.M <= 16)) return launch_few<F32, 1>(p, stream);
+    // Few outputs of more tokens, up to a workgroup per CU whose reads (32 rows of
+    // K) the next kernels' longer chains outlast (us, this and the next: 602 x 1152
+    // -> 32 4.9, 6.3; 1024 x 1152 -> 64 5.2, 6.5; beyond it 256 x 1152 -> 512 6.9,
+    // 6.6; 64 x 4608 -> 1152 18.6, 16.0; 285 x 2017 -> 17 12.3, 26.0).
+    const long long blocks = (long long)((p.N + 15) / 16) * ((p.M + 15) / 16);
+    if (blocks <= 256 && (!aligned || blocks * p.K <= 256 * 2304)) return launch_few<F32, 1>(p, stream);
     if (narrow && p.M <= 32 && (!aligned || p.K <= 2304)) return launch_few<F32, 2>(p, stream);
+    // 64 x 1001 -> 1153 9.0 us against 16.1, 200 tokens 15.0 and 16.6, 9436 x 2062 -> 16 20.1 and 33.1
+    if (!aligned && (long long)((p.N + 15) / 16) * ((p.M + 31) / 32) <= 512) return launch_few<F32, 2>(p, stream);
     const bool tail = p.K % (2 * GK) != 0;
     if (p.H > 1) return tail ? launch_tiles<ACT_HEADS_TAIL, F32>(p, stream) : launch_tiles<ACT_HEADS, F32>(p, stream);
     if (aligned) return tail ? launch_tiles<ACT_ROWS_TAIL, F32>(p, stream) : launch_tiles<ACT_ROWS, F32>(p, stream);

@@ -253,7 +253,11 @@ def _route(B, L, K, N, heads=1):
     narrow = K % 8 != 0 or N <= 4096
     if M <= 4 or (narrow and M <= 16):
         return "few 16"
+    if t(16, 16) <= 256 and (K % 8 or t(16, 16) * K <= 256 * 2304):
+        return "few 16"
     if narrow and M <= 32 and (K % 8 or K <= 2304):
+        return "few 32"
+    if K % 8 and t(16, 32) <= 512:
         return "few 32"
     if K % 8:
         return "any 64" if t(128, 128) <= 128 else "any 128"
@@ -270,13 +274,16 @@ def _route(B, L, K, N, heads=1):
 
 
 @pytest.mark.parametrize("B,L,K,N,heads,route", [
-    (1, 4, 1152, 6912, 1, "few 16"), (2, 8, 72, 40, 1, "few 16"), (2, 8, 77, 40, 1, "few 16"), (2, 15, 2304, 100, 1, "few 32"),
-    (2, 16, 9, 5000, 1, "few 32"), (1, 32, 5000, 64, 1, "64 ring"), (1, 5, 1152, 6912, 1, "64 ring"), (2, 150, 136, 515, 1, "64 ring"),
-    (2, 1100, 128, 1030, 1, "128 ring"), (2, 1100, 1000, 1030, 1, "128 ring"), (3, 100, 999, 333, 1, "any 64"), (1, 3000, 129, 901, 1, "any 128"),
+    (1, 4, 1152, 6912, 1, "few 16"), (2, 8, 72, 40, 1, "few 16"), (2, 8, 77, 40, 1, "few 16"), (2, 15, 2304, 100, 1, "few 16"),
+    (2, 16, 9, 5000, 1, "few 32"), (1, 32, 5000, 64, 1, "few 16"), (1, 5, 1152, 6912, 1, "64 ring"), (2, 150, 136, 515, 1, "64 ring"),
+    (2, 1100, 128, 1030, 1, "128 ring"), (2, 1100, 1000, 1030, 1, "128 ring"), (3, 100, 999, 333, 1, "few 32"), (1, 3000, 129, 901, 1, "any 128"),
     (2, 6000, 128, 1100, 1, "128"), (12, 1000, 328, 1099, 1, "128"), (1, 8200, 128, 1160, 1, "192"), (1, 8200, 136, 1153, 1, "192"),
     (1, 16100, 384, 2041, 1, "256"), (1, 16128, 128, 2048, 1, "256"), (2, 1100, 128, 1030, 2, "128 ring"), (12, 1000, 320, 1100, 5, "128"),
     (3, 2700, 192, 1160, 3, "192"), (1, 8200, 1152, 1153, 16, "192"), (2, 150, 216, 515, 3, "64 ring"),
-    (1, 1790, 136, 1150, 1, "64 ring"), (3, 596, 216, 1150, 3, "64 ring"), (1, 1793, 136, 1153, 1, "128 ring")])
+    (1, 1790, 136, 1150, 1, "64 ring"), (3, 596, 216, 1150, 3, "64 ring"), (1, 1793, 136, 1153, 1, "128 ring"),
+    (1, 30, 2304, 4000, 1, "few 32"), (3, 100, 999, 1333, 1, "any 64"), (1, 285, 2017, 17, 1, "few 16"),
+    (2, 301, 1152, 32, 1, "few 16"), (1, 64, 1001, 1153, 1, "few 32"), (1, 9000, 2062, 16, 1, "few 32"),
+    (1, 130, 1152, 200, 16, "few 16")])
 def test_linear_routes(B, L, K, N, heads, route):
     assert _route(B, L, K, N, heads) == route, "not the route this case is for"
     for ytype in (BF16, F32):
