@@ -353,16 +353,17 @@ constexpr int FORWARD_ROWS = 4;  // forward
 // group's tokens in the backward pass.  A workgroup per CU and 2 rows per
 // wavefront at least: more workgroups leave more partial sums (8192 tokens x
 // 1152, bf16: 256 workgroups of eight wavefronts 19.0 us, 512 of eight 23.0, 512
-// of four 19.2, 768 of four 20.0).  Two per CU up to 256 features, whose rows
-// are so short that latency counts (30798 x 191: 1 per CU 22, 2 18.0, 4 17.8 us;
-// 20000 x 64 12.6, 11.3, 14.2; 16000 x 512 17.7, 21 with 2).
+// of four 19.2, 768 of four 20.0).  Two per CU for many rows of up to 256
+// features, which are so short that latency counts (30798 x 191: 1 per CU 22, 2
+// 18.0, 4 17.8 us; 20000 x 64 12.6, 11.3, 14.2; but 16000 x 512 17.7, 21 with 2,
+// 9000 x 256 12.2, 12.6, and 5214 x 161 8.5, 10.1).
 struct Split {
     int rows, splits;
 };
 Split grad_split(int B, int L, int C, int groups) {
     const long long group_rows = (long long)B * L / groups;
     const int block = C <= WIDE ? GRAD_ROWS : 1;
-    const int slots = C <= 256 ? 512 : 256;
+    const int slots = C <= 256 && (long long)B * L >= 16384 ? 512 : 256;
     long long splits = (slots + groups - 1) / groups;
     long long rows = (group_rows + splits * block - 1) / (splits * block);
     if (rows < 2) rows = 2;

@@ -27,7 +27,7 @@ EPS = 1e-6
 # ends of what a wavefront and a workgroup hold; few and many tokens
 SHAPES = [(1, 1, 1), (1, 1, 64), (2, 3, 7), (2, 5, 512), (3, 2, 513), (3, 57, 777), (1, 3, 1279), (2, 4, 1280), (2, 301, 1152),
           (1, 9, 1281), (1, 2, 2048), (2, 3, 2049), (1, 5, 4096), (1, 5, 4097), (2, 2, 16384), (1, 4500, 130), (9, 1000, 64),
-          (1, 9000, 256), (2, 1100, 250), (1, 2100, 257)]
+          (1, 9000, 256), (2, 1100, 250), (1, 2100, 257), (2, 8500, 122)]
 
 
 def _inputs(B, L, C, dtype, affine, seed, offset=0.0, slices=True):
