@@ -313,9 +313,11 @@ __global__ void __launch_bounds__(512) linear_few_kernel(LinearParams p) {
 //   128 x 128, stream  two workgroups per CU; a last round of one takes 0.65
 //   192 x 256, stream  1.38 of its round for 1.5 of its output
 //   256 x 256, stream  1.76 for 2, K a multiple of 128 (the others' registers
-//                      spill); not for a single round, whose output nothing
-//                      runs beside (12960 x 1152 -> 1152 with an fp32 residual:
-//                      73 us against 65 by 128 x 128)
+//                      spill); nothing runs beside a single round's output, which
+//                      counts the more the fewer k-tiles there are (by 256 and 128, fp32
+//                      residual: 12960 x 1152 -> 1152 70, 64 us, 6000 x 1152 -> 2304 66,
+//                      66, 6000 x 2304 -> 2304 93, 98, 6000 x 4608 -> 2304 140, 151;
+//                      bf16: 8000 x 1152 -> 1664 44, 48, 12000 x 1920 -> 1152 69, 78)
 // us by 128, 192, 256: 32768 x 1152 -> 4608 396, 364, 342; 32768 x 4608 -> 1152
 // 360, 330, 353; 8192 x 1152 -> 4608 105, 103, 109.
 // Block order: the 32 or 64 workgroups that an XCD has resident share the lines
@@ -338,7 +340,7 @@ hipError_t launch_tiles(LinearParams& p, hipStream_t stream) {
     if (n128 <= 256) return launch_shape<ACT, LinearOut<F32, Tile128Ring>, Tile128Ring>(p, stream);
     const long long last = n128 % 512, rounds192 = (tiles<Tile192>(p) + 255) / 256, rounds256 = (tiles<Tile256>(p) + 255) / 256;
     const long long cost128 = 100 * (n128 / 512) + (last == 0 ? 0 : (last <= 256 ? 65 : 100)), cost192 = 138 * rounds192;
-    const long long cost256 = rounds256 > 1 ? 176 * rounds256 : cost128;
+    const long long cost256 = 176 * rounds256 + (rounds256 > 1 ? 0 : (F32 ? 32000 : 6000) / p.K);
     if constexpr (ACT == ACT_ROWS) {
         if (cost256 < cost128 && cost256 < cost192) {
             p.group = 3;

@@ -247,7 +247,7 @@ def test_another_device_is_refused(monkeypatch):
 
 
 # the routes of the linear layer: every tile, with a ragged last tile of either kind
-def _route(B, L, K, N, heads=1):
+def _route(B, L, K, N, heads=1, ytype=F32):
     M = B * L
     t = lambda f, k: -(-N // f) * -(-M // k)  # noqa: E731
     narrow = K % 8 != 0 or N <= 4096
@@ -268,7 +268,7 @@ def _route(B, L, K, N, heads=1):
         return "128 ring"
     c128 = 100 * (n // 512) + (0 if n % 512 == 0 else 65 if n % 512 <= 256 else 100)
     c192, r256 = 138 * -(-t(192, 256) // 256), -(-t(256, 256) // 256)
-    if heads == 1 and K % 128 == 0 and r256 > 1 and 176 * r256 < min(c128, c192):
+    if heads == 1 and K % 128 == 0 and 176 * r256 + ((32000 if ytype == F32 else 6000) // K if r256 == 1 else 0) < min(c128, c192):
         return "256"
     return "128" if c128 <= c192 else "192"
 
@@ -283,7 +283,7 @@ def _route(B, L, K, N, heads=1):
     (1, 1790, 136, 1150, 1, "64 ring"), (3, 596, 216, 1150, 3, "64 ring"), (1, 1793, 136, 1153, 1, "128 ring"),
     (1, 30, 2304, 4000, 1, "few 32"), (3, 100, 999, 1333, 1, "any 64"), (1, 285, 2017, 17, 1, "few 16"),
     (2, 301, 1152, 32, 1, "few 16"), (1, 64, 1001, 1153, 1, "few 32"), (1, 9000, 2062, 16, 1, "few 32"),
-    (1, 130, 1152, 200, 16, "few 16")])
+    (1, 130, 1152, 200, 16, "few 16"), (1, 5900, 2432, 2300, 1, "256")])
 def test_linear_routes(B, L, K, N, heads, route):
     assert _route(B, L, K, N, heads) == route, "not the route this case is for"
     for ytype in (BF16, F32):
